@@ -302,6 +302,109 @@ ditango_status ditango_state_norms(
     float* norms, void* workspace, void* stream);
 
 /*
+ * Cross attention: the query block attends to an encoder's states, a sequence
+ * of another length (the operator that follows the self attention in a DiT
+ * block).  For every batch b, token t and head h, over the live keys c of
+ * sequence b, with the key/value head hk = h / (H / Hk):
+ *     LSE[b][h][t] = log sum_c exp(scale * q[b][t][h] . k[b][c][hk])
+ *     OUT[b][t][h] = sum_c exp(scale * q . k_c - LSE) * v[b][c][hk]
+ * A state like the others (Eq. attention_state): it composes with them.
+ *
+ *   q, k, v      device; dtype `dt`; rows of D elements at the strides given
+ *                (host, 3 int64 each: elements between batches, tokens and
+ *                heads; 0 repeats, so that one sequence can serve a batch).
+ *                Addresses and strides are multiples of 16 bytes, and the
+ *                strides between tokens of k and v below 2^24 elements
+ *                (DITANGO_ERR_UNSUPPORTED otherwise).  k and v may be null
+ *                when kv_len is 0.
+ *   H, Hk        query heads, key/value heads; H a multiple of Hk.
+ *   D            64 or 128.
+ *   q_len        at least 1; q_len * H below 2^31 - 1024.
+ *   kv_len       keys of a sequence, 0 or more.
+ *   kv_lens      device, [B] int32: the live keys of a sequence are its first
+ *                kv_lens[b] (clamped to 0 ... kv_len); null: all.
+ *   key_mask     device, [B][kv_len] bytes, non-zero = live; null: all.  With
+ *                kv_lens both hold.
+ *   out          device, [B][q_len][H][D] in dtype `dt`, 16-byte aligned.
+ *   lse          device, [B][H][q_len] float32, or null.
+ *   workspace    device, 256-byte aligned, ditango_cross_attn_workspace_bytes
+ *                bytes; contents do not matter before or after.  A call with
+ *                key_mask needs it; one without key_mask and less workspace
+ *                (or none) runs, without splitting the keys of a short query
+ *                block over workgroups.  Calls that may overlap need one each.
+ *
+ * What lies in K and V at keys that are not live is never used, NaN included;
+ * a row without live keys has OUT = 0 and LSE = -inf.  Results do not depend
+ * on the order in which workgroups run.
+ */
+ditango_status ditango_cross_attn(
+    const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
+    const void* v, const int64_t* v_strides, ditango_dtype dt,
+    int B, int H, int Hk, int D, int64_t q_len, int64_t kv_len,
+    const int32_t* kv_lens, const uint8_t* key_mask, float scale,
+    void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace of ditango_cross_attn on the current device; `masked` as a call
+ * with key_mask.  0 for sizes that it rejects. */
+size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk, int D, int64_t q_len,
+                                          int64_t kv_len, int masked);
+
+/*
+ * Rotary positions of queries and keys, with the root-mean-square norm that
+ * precedes them: what makes the Q and K of the attention calls from those of
+ * the projections.  For every token and head, with x the row of D elements,
+ *     x^ = x, or x * rsqrt(mean(x^2) + eps) * weight
+ * with the mean over the row (DITANGO_NORM_HEAD) or over all heads of the
+ * token (DITANGO_NORM_ROW), and for the pairs i < rot_dim / 2 of its first
+ * rot_dim elements, at the angle a = positions[axis[i]] * freqs[i],
+ *     y0 = factor * (x^0 cos a - x^1 sin a),  y1 = factor * (x^0 sin a + x^1 cos a)
+ * where a pair's elements are 2i and 2i + 1 (DITANGO_ROTARY_INTERLEAVED) or i
+ * and i + rot_dim / 2 (DITANGO_ROTARY_HALF).  The others are x^.  Angles are
+ * formed and reduced in float64, the rest is float32, rounded once.
+ *
+ *   tensors      host, n_tensors (1 or 2: queries and keys of the same tokens)
+ *                descriptions: x and y device, dtype `dt`, rows of D elements
+ *                at the strides given (elements); y may be x (same strides),
+ *                but may not overlap it otherwise.  weight device, dtype `dt`,
+ *                [D] (HEAD) or [heads][D] (ROW); unused without a norm.
+ *                heads * D at most 65536.
+ *   positions    device, int32 [pos_batches][S][n_axes], pos_batches 1 or B.
+ *   freqs, axis  host, rot_dim / 2 each: radians per position (finite) and the
+ *                axis (below n_axes) of a pair.
+ *   rot_dim      even, 2 ... D.
+ *   D            64 or 128.
+ * Rows that are multiples of 16 bytes apart and aligned are read 16 bytes at a
+ * time, others 8 bytes or an element at a time.
+ */
+typedef enum {
+  DITANGO_ROTARY_INTERLEAVED = 0,
+  DITANGO_ROTARY_HALF = 1
+} ditango_rotary_layout;
+
+typedef enum {
+  DITANGO_NORM_NONE = 0,
+  DITANGO_NORM_HEAD = 1,
+  DITANGO_NORM_ROW = 2
+} ditango_rotary_norm;
+
+#define DITANGO_ROTARY_MAX_PAIRS 64
+#define DITANGO_ROTARY_MAX_AXES 8
+
+typedef struct {
+  const void* x;
+  void* y;
+  const void* weight;
+  int64_t x_strides[3];   /* between batches, tokens, heads */
+  int64_t y_strides[3];
+  int heads;
+} ditango_rotary_tensor;
+
+ditango_status ditango_rotary(
+    const ditango_rotary_tensor* tensors, int n_tensors, ditango_dtype dt, int B, int64_t S, int D,
+    const int32_t* positions, int pos_batches, int n_axes, const double* freqs, const uint8_t* axis, int rot_dim,
+    ditango_rotary_layout layout, float factor, ditango_rotary_norm norm, float eps, void* stream);
+
+/*
  * Device characterisation, not part of the method: the dense bf16 MFMA rate
  * the GPU sustains at the clock it runs at under MFMA load, to hold the
  * attention kernel against beside the published peak.  Launches

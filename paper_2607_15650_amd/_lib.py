@@ -18,6 +18,16 @@ F32, BF16 = 0, 1
 MAX_PARTITIONS = 64
 CONTRIB_SCRATCH_BYTES = 1 << 20
 
+# layouts and norms of ditango_rotary
+ROTARY_INTERLEAVED, ROTARY_HALF = 0, 1
+NORM_NONE, NORM_HEAD, NORM_ROW = 0, 1, 2
+
+
+class RotaryTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("x_strides", ctypes.c_int64 * 3), ("y_strides", ctypes.c_int64 * 3), ("heads", ctypes.c_int)]
+
+
 # Every symbol include/ditango.h declares, with (restype, argtypes).
 _c = ctypes
 SIGNATURES = {
@@ -69,6 +79,18 @@ SIGNATURES = {
         _c.c_void_p, _c.c_int, _c.c_int, _c.POINTER(_c.c_int32), _c.c_int,
         _c.c_int, _c.c_int, _c.c_int, _c.c_int64, _c.c_void_p,
         _c.c_void_p, _c.c_void_p, _c.c_void_p]),
+    "ditango_cross_attn": (_c.c_int, [
+        _c.c_void_p, _c.POINTER(_c.c_int64), _c.c_void_p, _c.POINTER(_c.c_int64),
+        _c.c_void_p, _c.POINTER(_c.c_int64), _c.c_int,
+        _c.c_int, _c.c_int, _c.c_int, _c.c_int, _c.c_int64, _c.c_int64,
+        _c.c_void_p, _c.c_void_p, _c.c_float,
+        _c.c_void_p, _c.c_void_p, _c.c_void_p, _c.c_size_t, _c.c_void_p]),
+    "ditango_cross_attn_workspace_bytes": (_c.c_size_t, [
+        _c.c_int, _c.c_int, _c.c_int, _c.c_int, _c.c_int, _c.c_int64, _c.c_int64, _c.c_int]),
+    "ditango_rotary": (_c.c_int, [
+        _c.POINTER(RotaryTensor), _c.c_int, _c.c_int, _c.c_int, _c.c_int64, _c.c_int,
+        _c.c_void_p, _c.c_int, _c.c_int, _c.POINTER(_c.c_double), _c.POINTER(_c.c_uint8), _c.c_int,
+        _c.c_int, _c.c_float, _c.c_int, _c.c_float, _c.c_void_p]),
     "ditango_probe_mfma_bf16": (_c.c_int, [_c.c_int, _c.c_int, _c.c_void_p, _c.c_void_p]),
     "ditango_status_string": (_c.c_char_p, [_c.c_int]),
     "ditango_version": (_c.c_char_p, []),

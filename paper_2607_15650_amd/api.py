@@ -47,6 +47,24 @@ def _dev(*ts: torch.Tensor) -> None:
         raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
 
 
+def _dev_strided(*ts: torch.Tensor) -> None:
+    """_dev for tensors whose rows lie apart (only the last dim is dense)."""
+    dev = None
+    for t in ts:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("all tensors must be on the GPU")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("all tensors must be on one device")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError("the elements of a row must be contiguous")
+    if dev is not None and dev.index != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
+
+
 def _stream() -> int:
     # the handle alone: the Stream object around it takes 2.8 us of every
     # call, this 0.3, and a small step is bound by its host work
@@ -287,6 +305,113 @@ def state_norms(out_states: torch.Tensor, norms: torch.Tensor, workspace: torch.
         out_states.data_ptr(), _dtype(out_states), P, sl, n, B, H, D, q_len,
         ref.data_ptr() if ref is not None else None, norms.data_ptr(), workspace.data_ptr(), _stream())
     _lib.check("ditango_state_norms", st)
+
+
+_I3 = ctypes.c_int64 * 3
+_DIMS = (64, 128)
+
+
+def cross_attn_workspace_bytes(dtype: torch.dtype, B: int, H: int, Hk: int, D: int, q_len: int, kv_len: int,
+                               masked: bool = False) -> int:
+    """Workspace bytes of cross_attn at these sizes on the current device."""
+    return int(_lib.lib().ditango_cross_attn_workspace_bytes(_DT[dtype], B, H, Hk, D, q_len, kv_len,
+                                                             1 if masked else 0))
+
+
+def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, out: torch.Tensor,
+               lse: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None,
+               key_mask: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Attention of q [B, q_len, H, D] to the states k, v [B, kv_len, Hk, D] of
+    an encoder, H a multiple of Hk (ditango_cross_attn), into ``out`` [B, q_len,
+    H, D] and ``lse`` [B, H, q_len].  q, k and v may be views with rows of their
+    own distance (a packed projection); addresses and strides are multiples of
+    16 bytes.  ``kv_lens`` int32 [B]: the live keys of a sequence are its first
+    ones; ``key_mask`` bool or uint8 [B, kv_len], non-zero = live.  A masked call
+    needs a ``workspace`` (uint8, 256-byte aligned) of
+    cross_attn_workspace_bytes(...) bytes, another one splits the keys of a short
+    query block with it."""
+    _dev_strided(q, k, v)
+    _dev(out, lse, kv_lens, key_mask, workspace)
+    if out.device != q.device:
+        raise ValueError("all tensors must be on one device")
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must be [B, tokens, heads, D]")
+    B, q_len, H, D = q.shape
+    _, kv_len, Hk, _ = k.shape
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+        raise ValueError("k/v shape mismatch")
+    if Hk < 1 or H % Hk:
+        raise ValueError("the query heads must be a multiple of the key/value heads")
+    if k.dtype != q.dtype or v.dtype != q.dtype or out.dtype != q.dtype:
+        raise ValueError("q, k, v and out must share a dtype")
+    if out.shape != q.shape:
+        raise ValueError("out must be [B, q_len, H, D]")
+    if lse is not None and (tuple(lse.shape) != (B, H, q_len) or lse.dtype != torch.float32):
+        raise ValueError("lse must be float32 [B, H, q_len]")
+    if kv_lens is not None and (tuple(kv_lens.shape) != (B,) or kv_lens.dtype != torch.int32):
+        raise ValueError("kv_lens must be int32 [B]")
+    if key_mask is not None and (tuple(key_mask.shape) != (B, kv_len) or
+                                 key_mask.dtype not in (torch.bool, torch.uint8)):
+        raise ValueError("key_mask must be bool or uint8 [B, kv_len]")
+    if key_mask is not None and kv_len > 0:
+        need = cross_attn_workspace_bytes(q.dtype, B, H, Hk, D, q_len, kv_len, True)
+        if workspace is None or workspace.numel() * workspace.element_size() < need:
+            raise ValueError(f"workspace too small: need {need} bytes")
+    ws, n = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+    st = _lib.lib().ditango_cross_attn(
+        q.data_ptr(), _I3(*q.stride()[:3]), k.data_ptr(), _I3(*k.stride()[:3]), v.data_ptr(), _I3(*v.stride()[:3]),
+        _dtype(q), B, H, Hk, D, q_len, kv_len,
+        kv_lens.data_ptr() if kv_lens is not None else None, key_mask.data_ptr() if key_mask is not None else None,
+        float(scale), out.data_ptr(), lse.data_ptr() if lse is not None else None, ws, n, _stream())
+    _lib.check("ditango_cross_attn", st)
+
+
+def rotary_tables(freqs: Sequence[float], axis: Sequence[int]):
+    """The host tables of ``rotary``: radians per position and axis of every pair."""
+    if len(freqs) != len(axis):
+        raise ValueError("freqs and axis must have one entry per pair")
+    return (ctypes.c_double * len(freqs))(*freqs), (ctypes.c_uint8 * len(axis))(*axis)
+
+
+def rotary(xs: Sequence[torch.Tensor], ys: Sequence[torch.Tensor], positions: torch.Tensor, tables, rot_dim: int,
+           layout: int, factor: float = 1.0, norm: int = _lib.NORM_NONE,
+           weights: Sequence[Optional[torch.Tensor]] = (None, None), eps: float = 1e-6) -> None:
+    """Rotary positions of one or two tensors [B, S, heads, D] of the same
+    tokens, after their root-mean-square norm if there is one (ditango_rotary).
+    ``ys`` may be ``xs``.  ``positions`` int32 [1 or B, S, axes]; ``tables`` from
+    rotary_tables; ``layout`` and ``norm`` as _lib names them; ``weights`` [D]
+    (of each head) or [heads * D] (of the token's row)."""
+    if not 1 <= len(xs) <= 2 or len(ys) != len(xs):
+        raise ValueError("one or two tensors, and an output for each")
+    _dev_strided(*xs, *ys)
+    _dev(positions, *weights[:len(xs)])
+    B, S, _, D = xs[0].shape
+    if positions.device != xs[0].device:
+        raise ValueError("all tensors must be on one device")
+    if positions.dtype != torch.int32 or positions.dim() != 3 or positions.shape[1] != S or \
+            positions.shape[0] not in (1, B):
+        raise ValueError("positions must be int32 [1 or B, S, axes]")
+    if len(tables[0]) * 2 != rot_dim:
+        raise ValueError("the tables must have one entry per pair of rot_dim")
+    arr = (_lib.RotaryTensor * len(xs))()
+    for i, (x, y) in enumerate(zip(xs, ys)):
+        if x.dim() != 4 or x.shape[0] != B or x.shape[1] != S or x.shape[3] != D or y.shape != x.shape:
+            raise ValueError("tensors must be [B, S, heads, D] of the same tokens, outputs like them")
+        if x.dtype != xs[0].dtype or y.dtype != x.dtype:
+            raise ValueError("the tensors must share a dtype")
+        w = weights[i] if norm != _lib.NORM_NONE else None
+        if norm != _lib.NORM_NONE:
+            need = D if norm == _lib.NORM_HEAD else x.shape[2] * D
+            if w is None or w.numel() != need or w.dtype != x.dtype:
+                raise ValueError(f"the norm needs {need} weights in the input dtype")
+        a = arr[i]
+        a.x, a.y, a.weight = x.data_ptr(), y.data_ptr(), w.data_ptr() if w is not None else None
+        a.x_strides[:], a.y_strides[:] = x.stride()[:3], y.stride()[:3]
+        a.heads = x.shape[2]
+    st = _lib.lib().ditango_rotary(
+        arr, len(xs), _dtype(xs[0]), B, S, D, positions.data_ptr(), positions.shape[0], positions.shape[2],
+        tables[0], tables[1], rot_dim, layout, factor, norm, eps, _stream())
+    _lib.check("ditango_rotary", st)
 
 
 def probe_mfma_bf16(n_workgroups: int, iters: int, sink: torch.Tensor) -> float:

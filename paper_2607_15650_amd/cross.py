@@ -1,0 +1,57 @@
+"""Cross attention to an encoder's states, the operator after the self
+attention in a DiT block.  All work runs in the HIP kernels behind the C ABI;
+this module owns the workspace and the outputs.
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import api
+
+
+def _rows(x: torch.Tensor) -> torch.Tensor:
+    """``x`` itself where the kernels read it in place (rows of contiguous
+    elements, addresses and strides of 16 bytes), or a dense copy."""
+    e = x.element_size()
+    s0, s1, s2, s3 = x.stride()
+    if s3 == 1 and not (x.data_ptr() | s0 * e | s1 * e | s2 * e) & 15:
+        return x
+    return x.clone(memory_format=torch.contiguous_format)
+
+
+class CrossAttention:
+    """Attention of query blocks to encoder states, with the workspace kept
+    across calls (it only grows).  The calls of one instance share it: order
+    them on one stream, or across streams by events; a captured graph keeps the
+    workspace that was there when it was captured, so make the largest call
+    before the capture and no larger one until the graph is gone."""
+
+    def __init__(self, scale: float):
+        self.scale = float(scale)
+        self._ws: Optional[torch.Tensor] = None
+        self._bytes = {}
+
+    def _workspace(self, q, k, masked: bool) -> Optional[torch.Tensor]:
+        key = (q.dtype, q.shape, k.shape, masked, q.device)
+        n = self._bytes.get(key)
+        if n is None:
+            n = self._bytes[key] = api.cross_attn_workspace_bytes(
+                q.dtype, q.shape[0], q.shape[2], k.shape[2], q.shape[3], q.shape[1], k.shape[1], masked)
+        if n == 0:
+            return None
+        if self._ws is None or self._ws.numel() < n or self._ws.device != q.device:
+            self._ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+        return self._ws
+
+    def __call__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_lens: Optional[torch.Tensor] = None,
+                 key_mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(OUT [B, q_len, H, D], LSE [B, H, q_len]) of q [B, q_len, H, D] over the
+        live keys of k, v [B, kv_len, Hk, D].  Tensors that the kernels cannot
+        read in place are copied first."""
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        api.cross_attn(q, k, v, self.scale, out, lse, kv_lens, key_mask, self._workspace(q, k, key_mask is not None))
+        return out, lse

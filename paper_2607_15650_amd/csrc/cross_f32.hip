@@ -1,0 +1,184 @@
+// cross_f32.hip - the cross attention of cross.hip for float32 inputs
+// (gfx950): the key loop of attn_f32_loop.h (float32 products as six bf16
+// MFMAs) over rows that are strided or listed, and the same second pass with
+// the float32 MFMA where the planes cannot hold a value.
+//
+// A workgroup is four waves and 32 rows of one key/value head: the waves
+// split the keys of its range, stage their own tiles without barriers, and
+// compose their partial states through LDS.
+#include "attn_f32_loop.h"
+#include "internal.h"
+
+namespace ditango {
+namespace {
+
+template <class C, class Rows>
+__global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArgs a) {
+  constexpr int D = C::D;
+  static_assert(C::RW == 1 && C::KW > 1, "the waves split the keys");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+
+  int t = xcd_remap(blockIdx.x, gridDim.x);
+  const int rt = t % a.row_tiles;
+  t /= a.row_tiles;
+  const int sp = t % a.split;
+  t /= a.split;
+  const int hk = t % a.Hk;
+  const int b = t / a.Hk;
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, g = lane >> 5;
+
+  const int n = __builtin_amdgcn_readfirstlane(cross_keys(a, b));
+  const int all = (n + C::BN - 1) / C::BN;
+  const int tiles_per = (all + a.split - 1) / a.split;
+  const int tb = min(sp * tiles_per, all), te = min(tb + tiles_per, all);
+  const int kv_len = n;
+
+  Rows kr, vr;
+  kr.base = (const float*)a.k + b * a.k_batch + hk * a.k_head;
+  vr.base = (const float*)a.v + b * a.v_batch + hk * a.v_head;
+  kr.stride = a.k_token;
+  vr.stride = a.v_token;
+  if constexpr (Rows::kListed) kr.list = vr.list = a.list + (int64_t)b * a.kv_len;
+
+  const int row = rt * C::BM + lr;
+  const bool row_ok = row < a.rows;
+  const int tok = min(row, a.rows - 1) / a.G, gi = min(row, a.rows - 1) % a.G;
+  const float* qrow = (const float*)a.q + b * a.q_batch + tok * a.q_token + (int64_t)(hk * a.G + gi) * a.q_head;
+
+  const int per = (te - tb + C::KW - 1) / C::KW;
+  const int t0 = min(tb + wave * per, te), t1 = min(t0 + per, te);
+  unsigned char* kb = smem + wave * C::GROUP;
+  float* part_m = (float*)(smem + C::KW * C::GROUP);
+  float* part_l = part_m + C::KW * 32;
+  int* redo = (int*)(part_l + C::KW * 32);
+
+  f32x16 o[C::DB];
+  float m, l;
+  if (tid < 3) redo[tid] = 0;
+  uint64_t ask = 0;
+  key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, lane, o, m, l, ask);
+  // what the planes cannot hold, as attn_f32_kernel finds it
+  float bad = l * 0.f, low = INFINITY;
+#pragma unroll
+  for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      bad = __builtin_fmaf(o[db][r], 0.f, bad);
+      low = fminf(low, fabsf(o[db][r]));
+    }
+  const float below = pair_sum(l) * 0x1p-100f;
+  const bool small = row_ok && low < below;
+  __syncthreads();
+  if ((__builtin_amdgcn_ballot_w64(!(bad == 0.f)) | ask) != 0 && lane == 0) redo[0] = 1;
+  if (__builtin_amdgcn_ballot_w64(small) != 0 && lane == 0) redo[1] = 1;
+  __syncthreads();
+  bool again = __builtin_amdgcn_readfirstlane(redo[0]) != 0;
+  if (!again && __builtin_amdgcn_readfirstlane(redo[1]) != 0) {
+    constexpr int kBatch = 8;
+    const int first = tb * C::BN;
+    const int64_t units = (int64_t)(min(te * C::BN, n) - first) * (D / 4);
+    bool found = false;
+    for (int64_t i0 = tid; i0 < units; i0 += kBatch * C::NT) {
+      f32x4 x[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int64_t u = min(i0 + i * C::NT, units - 1);
+        x[i] = *(const f32x4*)(vr.row(first + (int)(u / (D / 4))) + u % (D / 4) * 4);
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) found |= below_planes(x[i][e]);
+    }
+    if (__builtin_amdgcn_ballot_w64(found) != 0 && lane == 0) redo[2] = 1;
+    __syncthreads();
+    again = __builtin_amdgcn_readfirstlane(redo[2]) != 0;
+  }
+  if (again) {
+    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, lane, o, m, l, ask);
+    __syncthreads();
+  }
+
+  // partial states through LDS: O rows of 16-byte units, swizzled by row
+  const float lt = pair_sum(l);
+  float* po = (float*)kb;
+#pragma unroll
+  for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      f32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = o[db][4 * r4 + e];
+      *(f32x4*)(po + lr * D + (((8 * db + 2 * r4 + g) ^ (lr & 15)) * 4)) = x;
+    }
+  if (g == 0) {
+    part_m[wave * 32 + lr] = m;
+    part_l[wave * 32 + lr] = lt;
+  }
+  __syncthreads();
+  constexpr int CH = 32 * D / 4;
+  static_assert(CH % C::NT == 0, "chunks divide over the threads");
+#pragma unroll
+  for (int i = 0; i < CH / C::NT; ++i) {
+    const int c = tid + i * C::NT;
+    const int r = c / (D / 4), u = c % (D / 4);
+    if (rt * C::BM + r >= a.rows) continue;
+    const int rtok = (rt * C::BM + r) / a.G, h = hk * a.G + (rt * C::BM + r) % a.G;
+    float mk[C::KW], M = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < C::KW; ++k) {
+      mk[k] = part_m[k * 32 + r];
+      M = fmaxf(M, mk[k]);
+    }
+    float tot = 0.f;
+    f32x4 acc = f32x4{};
+#pragma unroll
+    for (int k = 0; k < C::KW; ++k) {
+      const float w = mk[k] == -INFINITY && part_l[k * 32 + r] == 0.f ? 0.f : fast_exp2(mk[k] - M);
+      tot = __builtin_fmaf(w, part_l[k * 32 + r], tot);
+      acc += w * *(const f32x4*)((const float*)(smem + k * C::GROUP) + r * D + ((u ^ (r & 15)) * 4));
+    }
+    const float inv = tot > 0.f ? 1.0f / tot : 0.f;
+    const float lse = tot > 0.f ? (M + __builtin_amdgcn_logf(tot)) * kLn2 : tot == 0.f ? -INFINITY : tot;
+    const int64_t at = ((int64_t)b * a.H + h) * a.q_len + rtok;
+    if (a.split > 1) {
+      const int64_t ap = (int64_t)sp * a.B * a.H * a.q_len + at;
+      *(f32x4*)(a.part_out + ap * D + u * 4) = acc * inv;
+      if (u == 0) a.part_lse[ap] = lse;
+    } else {
+      *(f32x4*)((float*)a.out + (((int64_t)b * a.q_len + rtok) * a.H + h) * D + u * 4) = acc * inv;
+      if (u == 0 && a.lse != nullptr) a.lse[at] = lse;
+    }
+  }
+}
+
+template <class C, class Rows>
+hipError_t launch_f32_rows(const CrossArgs& a0, hipStream_t s) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  e = set_kernel_lds<&cross_f32_kernel<C, Rows>, C::LDS>(dev);
+  if (e != hipSuccess) return e;
+  CrossArgs a = a0;
+  a.row_tiles = (a.rows + C::BM - 1) / C::BM;
+  const int64_t grid = (int64_t)a.row_tiles * a.split * a.Hk * a.B;
+  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((cross_f32_kernel<C, Rows>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int cross_f32_rows(int) { return 32; }
+
+hipError_t launch_cross_f32(const CrossArgs& a, int D, hipStream_t s) {
+  using C128 = CfgF<128, 1, 4, 1, false>;
+  using C64 = CfgF<64, 1, 8, 2, false>;
+  if (D == 128) return a.mask ? launch_f32_rows<C128, ListedRows>(a, s) : launch_f32_rows<C128, StridedRows>(a, s);
+  return a.mask ? launch_f32_rows<C64, ListedRows>(a, s) : launch_f32_rows<C64, StridedRows>(a, s);
+}
+
+}  // namespace ditango

@@ -335,6 +335,130 @@ ditango_status ditango_state_norms(
   return from_hip(launch_norms(a, dt, (hipStream_t)stream));
 }
 
+}  // extern "C"
+
+namespace {
+
+bool aligned16(const void* p, const int64_t* strides, int64_t bytes) {
+  if (((uintptr_t)p & 15u) != 0) return false;
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] * bytes % 16 != 0) return false;
+  return true;
+}
+
+// Argument checks of the cross attention that need the sizes only; fills them.
+ditango_status cross_sizes(ditango_dtype dt, int B, int H, int Hk, int D, int64_t q_len, int64_t kv_len, CrossArgs* a) {
+  if (!valid_dtype(dt)) return DITANGO_ERR_INVALID;
+  if (B < 1 || H < 1 || Hk < 1 || q_len < 1 || kv_len < 0 || H % Hk != 0) return DITANGO_ERR_INVALID;
+  if (D != 64 && D != 128) return DITANGO_ERR_UNSUPPORTED;
+  if (q_len > (0x7fffffffLL - 1024) / H || kv_len > 0x7fffffffLL - 1024) return DITANGO_ERR_UNSUPPORTED;
+  memset(a, 0, sizeof(*a));
+  a->q_len = q_len;
+  a->B = B;
+  a->H = H;
+  a->Hk = Hk;
+  a->G = H / Hk;
+  a->kv_len = (int)kv_len;
+  a->rows = (int)q_len * a->G;
+  return DITANGO_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ditango_status ditango_cross_attn(
+    const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
+    const void* v, const int64_t* v_strides, ditango_dtype dt,
+    int B, int H, int Hk, int D, int64_t q_len, int64_t kv_len,
+    const int32_t* kv_lens, const uint8_t* key_mask, float scale,
+    void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  CrossArgs a;
+  const ditango_status st = cross_sizes(dt, B, H, Hk, D, q_len, kv_len, &a);
+  if (st != DITANGO_OK) return st;
+  if (!q || !q_strides || !k_strides || !v_strides || !out || (kv_len > 0 && (!k || !v))) return DITANGO_ERR_INVALID;
+  // the running maximum is kept on scores scaled after it is taken
+  if (!isfinite(scale) || !(scale > 0.f)) return DITANGO_ERR_INVALID;
+  for (int i = 0; i < 3; ++i)
+    if (q_strides[i] < 0 || k_strides[i] < 0 || v_strides[i] < 0) return DITANGO_ERR_INVALID;
+  const int64_t e = dt == DITANGO_F32 ? 4 : 2;
+  if (!aligned16(q, q_strides, e) || !aligned16(k, k_strides, e) || !aligned16(v, v_strides, e) ||
+      ((uintptr_t)out & 15u) != 0)
+    return DITANGO_ERR_UNSUPPORTED;
+  // offsets inside a tile of keys are 32 bits
+  if (k_strides[1] >= (1 << 24) || v_strides[1] >= (1 << 24)) return DITANGO_ERR_UNSUPPORTED;
+  if (((uintptr_t)workspace & 255u) != 0) return DITANGO_ERR_INVALID;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.lse = lse;
+  a.q_batch = q_strides[0], a.q_token = q_strides[1], a.q_head = q_strides[2];
+  a.k_batch = k_strides[0], a.k_token = k_strides[1], a.k_head = k_strides[2];
+  a.v_batch = v_strides[0], a.v_token = v_strides[1], a.v_head = v_strides[2];
+  a.lens = kv_lens;
+  a.mask = kv_len > 0 ? key_mask : nullptr;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  if (a.mask != nullptr && (!workspace || workspace_bytes < cross_list_bytes(a))) return DITANGO_ERR_INVALID;
+  return from_hip(launch_cross(a, dt, D, workspace, workspace != nullptr ? workspace_bytes : 0, (hipStream_t)stream));
+}
+
+size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk, int D, int64_t q_len,
+                                          int64_t kv_len, int masked) {
+  CrossArgs a;
+  if (cross_sizes(dt, B, H, Hk, D, q_len, kv_len, &a) != DITANGO_OK) return 0;
+  static const uint8_t dummy[1] = {0};
+  a.mask = masked != 0 && kv_len > 0 ? dummy : nullptr;
+  CrossPlan p;
+  return plan_cross(a, dt, D, &p) == hipSuccess ? p.bytes : 0;
+}
+
+ditango_status ditango_rotary(
+    const ditango_rotary_tensor* tensors, int n_tensors, ditango_dtype dt, int B, int64_t S, int D,
+    const int32_t* positions, int pos_batches, int n_axes, const double* freqs, const uint8_t* axis, int rot_dim,
+    ditango_rotary_layout layout, float factor, ditango_rotary_norm norm, float eps, void* stream) {
+  if (!tensors || !positions || !freqs || !axis) return DITANGO_ERR_INVALID;
+  if (!valid_dtype(dt)) return DITANGO_ERR_INVALID;
+  if (n_tensors < 1 || n_tensors > 2 || B < 1 || S < 1) return DITANGO_ERR_INVALID;
+  if (pos_batches != 1 && pos_batches != B) return DITANGO_ERR_INVALID;
+  if (n_axes < 1 || n_axes > DITANGO_ROTARY_MAX_AXES) return DITANGO_ERR_INVALID;
+  if (layout != DITANGO_ROTARY_INTERLEAVED && layout != DITANGO_ROTARY_HALF) return DITANGO_ERR_INVALID;
+  if (norm != DITANGO_NORM_NONE && norm != DITANGO_NORM_HEAD && norm != DITANGO_NORM_ROW) return DITANGO_ERR_INVALID;
+  if (D != 64 && D != 128) return DITANGO_ERR_UNSUPPORTED;
+  if (rot_dim < 2 || rot_dim > D || rot_dim % 2 != 0) return DITANGO_ERR_INVALID;
+  if (!isfinite(factor)) return DITANGO_ERR_INVALID;
+  if (norm != DITANGO_NORM_NONE && !(eps >= 0.f && isfinite(eps))) return DITANGO_ERR_INVALID;
+  if (S > 0x7fffffffLL / B) return DITANGO_ERR_UNSUPPORTED;
+  RotaryArgs a;
+  memset(&a, 0, sizeof(a));
+  for (int i = 0; i < n_tensors; ++i) {
+    const ditango_rotary_tensor& t = tensors[i];
+    if (!t.x || !t.y || t.heads < 1 || (norm != DITANGO_NORM_NONE && !t.weight)) return DITANGO_ERR_INVALID;
+    if ((int64_t)t.heads * D > 65536) return DITANGO_ERR_UNSUPPORTED;
+    for (int k = 0; k < 3; ++k) {
+      if (t.x_strides[k] < 0 || t.y_strides[k] < 0) return DITANGO_ERR_INVALID;
+      // in place only where every element is read and written at one place
+      if (t.x == t.y && t.x_strides[k] != t.y_strides[k]) return DITANGO_ERR_INVALID;
+    }
+    a.t[i] = t;
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    if (!isfinite(freqs[i]) || axis[i] >= n_axes) return DITANGO_ERR_INVALID;
+    a.turns[i] = freqs[i] * 0.15915494309189535;   // 1 / 2 pi
+    a.axis[i] = axis[i];
+  }
+  a.n = n_tensors;
+  a.B = B;
+  a.S = S;
+  a.rot = rot_dim;
+  a.axes = n_axes;
+  a.pos = positions;
+  a.pos_batch = pos_batches == 1 ? 0 : S * n_axes;
+  a.factor = factor;
+  a.eps = eps;
+  return from_hip(launch_rotary(a, dt, D, layout, norm, (hipStream_t)stream));
+}
+
 ditango_status ditango_probe_mfma_bf16(int n_workgroups, int iters, float* sink, void* stream) {
   if (!sink || n_workgroups < 1 || iters < 1) return DITANGO_ERR_INVALID;
   if (n_workgroups > (1 << 20) || iters > (1 << 20)) return DITANGO_ERR_INVALID;

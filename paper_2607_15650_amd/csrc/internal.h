@@ -12,6 +12,15 @@ namespace ditango {
 
 constexpr int kMaxParts = DITANGO_MAX_PARTITIONS;
 
+// Dynamic LDS of a kernel, set once on every device.
+template <auto KERNEL, int BYTES>
+inline hipError_t set_kernel_lds(int dev) {
+  static OncePerDevice once;
+  return once.run(dev, [] {
+    return hipFuncSetAttribute((const void*)KERNEL, hipFuncAttributeMaxDynamicSharedMemorySize, BYTES);
+  });
+}
+
 // One launch of the fresh-state kernel covers every selected partition.
 struct AttnArgs {
   const void* q;            // [B][q_len][H][D], batches q_stride elements apart
@@ -189,6 +198,81 @@ hipError_t launch_contrib(const ContribArgs& a, hipStream_t s);
 constexpr size_t kContribScratchBytes = DITANGO_CONTRIB_SCRATCH_BYTES;
 hipError_t contrib_scratch(float** ptr);
 hipError_t launch_norms(const NormArgs& a, ditango_dtype dt, hipStream_t s);
+
+// One launch of the cross attention.  The rows of a key/value head are those
+// of the query heads that share it: row r is token r / G of head hk * G + r % G.
+// Strides are in elements.
+struct CrossArgs {
+  const void* q;            // rows of D elements, as the strides say
+  const void* k;
+  const void* v;
+  void* out;                // [B][q_len][H][D]
+  float* lse;               // [B][H][q_len] or null
+  int64_t q_batch, q_token, q_head;
+  int64_t k_batch, k_token, k_head;
+  int64_t v_batch, v_token, v_head;
+  int64_t q_len;
+  int B, H, Hk, G;
+  int kv_len;               // keys of a sequence, at most
+  int rows;                 // q_len * G
+  int row_tiles;            // ceil(rows / rows per workgroup)
+  int split;                // key ranges, each a workgroup's
+  float scale_log2;
+  const int32_t* lens;      // [B] live keys of a sequence (a prefix), or null
+  const uint8_t* mask;      // [B][kv_len] or null
+  // the masked form, in the workspace: the live keys' places in order
+  // [B][kv_len], how many they are [B], and a row of zeros
+  int32_t* list;
+  int32_t* count;
+  float* zeros;
+  // partial states of a split launch, in the workspace
+  float* part_out;          // [split][B][H][q_len][D]
+  float* part_lse;          // [split][B][H][q_len]
+};
+
+// Live keys of sequence b.
+__device__ __forceinline__ int cross_keys(const CrossArgs& a, int b) {
+  if (a.mask != nullptr) return a.count[b];
+  return a.lens == nullptr ? a.kv_len : min(max(a.lens[b], 0), a.kv_len);
+}
+
+// How a launch of the cross attention runs on the current device, and the
+// workspace it takes.
+inline size_t align_up256(size_t x) { return (x + 255) & ~(size_t)255; }
+// of a masked call: the list, the counts and the zeros
+inline size_t cross_list_bytes(const CrossArgs& a) {
+  return a.mask == nullptr ? 0 : align_up256((size_t)a.B * a.kv_len * 4) + align_up256((size_t)a.B * 4) + 512;
+}
+struct CrossPlan {
+  int split;
+  size_t bytes;             // with the partial states: without room for them the launch is not split
+};
+hipError_t plan_cross(const CrossArgs& a, ditango_dtype dt, int D, CrossPlan* p);
+hipError_t launch_cross(const CrossArgs& a, ditango_dtype dt, int D, void* ws, size_t ws_bytes, hipStream_t s);
+hipError_t launch_cross_f32(const CrossArgs& a, int D, hipStream_t s);
+int cross_f32_rows(int D);  // rows per workgroup
+
+// One launch of the rotary positions.
+struct RotaryArgs {
+  ditango_rotary_tensor t[2];
+  int n;                    // tensors
+  int B;
+  int64_t S;
+  int rot;                  // rotated dims
+  int axes;
+  const int32_t* pos;       // [1 or B][S][axes]
+  int64_t pos_batch;        // 0, or S * axes
+  float factor;             // of cosine and sine
+  float eps;
+  // the launch: a team of threads per token
+  int team;
+  int units[2];             // of a token of each tensor
+  double turns[DITANGO_ROTARY_MAX_PAIRS];    // of a pair, per position
+  uint8_t axis[DITANGO_ROTARY_MAX_PAIRS];
+};
+// vec: elements of a load, as alignment and sizes allow
+hipError_t launch_rotary(const RotaryArgs& a, ditango_dtype dt, int D, ditango_rotary_layout layout,
+                         ditango_rotary_norm norm, hipStream_t s);
 
 constexpr int kProbeThreads = 256;   // 4 waves per workgroup
 hipError_t launch_probe_mfma(int n_workgroups, int iters, float* sink, hipStream_t s);

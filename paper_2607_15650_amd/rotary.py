@@ -1,0 +1,118 @@
+"""Rotary positions of queries and keys, and the root-mean-square norm before
+them: what makes the attention's inputs from those of the projections.  The
+kernel is behind the C ABI (ditango_rotary); this module computes the
+frequencies, which depend on the configuration only.
+"""
+from __future__ import annotations
+
+import math
+from typing import Dict, List, Optional, Sequence, Tuple
+
+import torch
+
+from . import _lib, api
+
+_LAYOUT = {"interleaved": _lib.ROTARY_INTERLEAVED, "half": _lib.ROTARY_HALF}
+_NORM = {"none": _lib.NORM_NONE, "head": _lib.NORM_HEAD, "row": _lib.NORM_ROW}
+
+
+def axis_frequencies(dim: int, theta: float = 10000.0, scaling: Optional[Dict] = None) -> Tuple[List[float], float]:
+    """Radians per position of the dim / 2 pairs of one axis, and the factor of
+    cosine and sine.  theta^(-2i / dim), scaled for positions beyond those of
+    the training (``scaling``: {"kind", "factor": s, ...}):
+      linear  every frequency by 1 / s;
+      ntk     theta by s^(dim / (dim - 2)): the lowest by 1 / s, the highest kept;
+      yarn    (arXiv 2309.00071) by how often a pair turns over the ``original``
+              positions: kept from ``beta`` turns on (32), by 1 / s up to
+              ``alpha`` (1), linear between; cosine and sine by 0.1 ln s + 1.
+    """
+    if dim < 2 or dim % 2:
+        raise ValueError("an axis takes an even number of dims, 2 at least")
+    s, kind, factor = 1.0, "none", 1.0
+    if scaling is not None:
+        kind, s = scaling["kind"], float(scaling["factor"])
+        if kind not in ("linear", "ntk", "yarn"):
+            raise ValueError(f"unknown scaling {kind!r}; use linear, ntk or yarn")
+        if not s >= 1.0 or not math.isfinite(s):
+            raise ValueError("a scaling's factor is 1 at least")
+    if kind == "ntk":
+        if dim < 4:
+            raise ValueError("ntk scaling needs 4 dims at least")
+        theta = theta * s ** (dim / (dim - 2))
+    freqs = [theta ** (-2.0 * i / dim) for i in range(dim // 2)]
+    if kind == "linear":
+        freqs = [f / s for f in freqs]
+    elif kind == "yarn":
+        alpha, beta = float(scaling.get("alpha", 1.0)), float(scaling.get("beta", 32.0))
+        original = float(scaling["original"])
+        if not beta > alpha or not original > 0:
+            raise ValueError("yarn scaling needs beta above alpha and the original number of positions")
+        keep = [min(1.0, max(0.0, (original * f / (2 * math.pi) - alpha) / (beta - alpha))) for f in freqs]
+        freqs = [f * (g + (1.0 - g) / s) for f, g in zip(freqs, keep)]
+        factor = 0.1 * math.log(s) + 1.0
+    return freqs, factor
+
+
+def grid_positions(frames: int, rows: int, cols: int, first: int = 0, count: Optional[int] = None,
+                   device="cuda") -> torch.Tensor:
+    """Positions [1, count, 3] (frame, row, column) of tokens [first, first +
+    count) of a latent grid, flattened frame by frame."""
+    total = frames * rows * cols
+    count = total - first if count is None else count
+    if first < 0 or count < 0 or first + count > total:
+        raise ValueError("the tokens must lie inside the grid")
+    n = torch.arange(first, first + count, device=device)
+    return torch.stack([n // (rows * cols), n // cols % rows, n % cols], dim=-1).to(torch.int32)[None].contiguous()
+
+
+class Rotary:
+    """Rotary positions of a layer's queries and keys.
+
+    ``axes``: the rotated dims of every axis of the positions (frame, row and
+    column of a latent grid, say), together at most ``head_dim``; the dims after
+    them are left as they are.  ``layout``: a pair's two elements are neighbours
+    ("interleaved") or half of the rotated dims apart ("half").  ``norm``: the
+    root-mean-square norm before the rotation, over each head ("head"), over all
+    heads of a token ("row"), or "none".  ``scaling`` as axis_frequencies takes
+    it, for every axis.
+    """
+
+    def __init__(self, head_dim: int, axes: Optional[Sequence[int]] = None, theta: float = 10000.0,
+                 layout: str = "interleaved", scaling: Optional[Dict] = None, norm: str = "none", eps: float = 1e-6):
+        axes = [head_dim] if axes is None else [int(a) for a in axes]
+        if layout not in _LAYOUT or norm not in _NORM:
+            raise ValueError("layout is interleaved or half; norm is none, head or row")
+        if not axes or sum(axes) > head_dim:
+            raise ValueError("the axes' dims must fit the head")
+        self.head_dim, self.axes = head_dim, axes
+        self.rot_dim, self.factor = sum(axes), 1.0
+        self.freqs: List[float] = []
+        self.axis: List[int] = []
+        for i, dim in enumerate(axes):
+            f, self.factor = axis_frequencies(dim, theta, scaling)
+            self.freqs += f
+            self.axis += [i] * (dim // 2)
+        self.layout, self.norm, self.eps = layout, norm, float(eps)
+        self._tables = api.rotary_tables(self.freqs, self.axis)
+
+    def __call__(self, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
+        """(q, k) rotated, or q alone where k is None: new dense tensors, or the
+        ones given (``q`` and ``k`` themselves to work in place).  q, k [B, S,
+        heads, head_dim] are the same tokens, at ``positions`` int32 [1 or B, S,
+        len(axes)]."""
+        if q.shape[-1] != self.head_dim:
+            raise ValueError(f"the rows must have {self.head_dim} elements")
+        if positions.dim() != 3 or positions.shape[2] != len(self.axes):
+            raise ValueError("positions must be int32 [1 or B, S, axes]")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        xs, ys = (q,), (q_out,)
+        if k is not None:
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            xs, ys = (q, k), (q_out, k_out)
+        api.rotary(xs, ys, positions, self._tables, self.rot_dim, _LAYOUT[self.layout], self.factor, _NORM[self.norm],
+                   (q_weight, k_weight), self.eps)
+        return (q_out, k_out) if k is not None else q_out
