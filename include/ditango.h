@@ -317,7 +317,8 @@ ditango_status ditango_state_norms(
  *                strides between tokens of k and v below 2^24 elements
  *                (DITANGO_ERR_UNSUPPORTED otherwise).  k and v may be null
  *                when kv_len is 0.
- *   H, Hk        query heads, key/value heads; H a multiple of Hk.
+ *   H, Hk        query heads (at most 32768), key/value heads; H a multiple of
+ *                Hk.
  *   D            64 or 128.
  *   q_len        at least 1; q_len * H below 2^31 - 1024.
  *   kv_len       keys of a sequence, 0 or more.

@@ -17,7 +17,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libditango.so")
 SOURCES = ["ditango_api.cpp", "attn_bf16.hip", "attn_bf16_any_q.hip", "attn_f32.hip", "merge.hip", "norms.hip", "cross.hip",
-           "cross_f32.hip", "rotary.hip", "probe.hip"]
+           "cross_f32.hip", "cross_task.hip", "cross_resident.hip",
+           "cross_few.hip", "rotary.hip", "probe.hip"]
 ARCH = "gfx950"
 # Per-source compiler options.  The attention kernel is scheduled with the
 # backend's iterative ILP strategy, which interleaves its MFMAs, LDS reads and
@@ -50,7 +51,10 @@ def flags():
 INCLUDES = {"attn_bf16.hip": ["attn_tile.h", "attn_d128_loop.inc", "attn_d64_loop.inc"],
             "attn_bf16_any_q.hip": ["attn_bf16.hip", "attn_tile.h", "attn_d128_loop.inc", "attn_d64_loop.inc"],
             "attn_f32.hip": ["attn_tile.h", "attn_f32_loop.h"],
-            "cross.hip": ["attn_tile.h"],
+            "cross.hip": ["attn_tile.h", "cross_tile.h"],
+            "cross_few.hip": ["attn_tile.h", "cross_tile.h"],
+            "cross_resident.hip": ["attn_tile.h", "cross_tile.h"],
+            "cross_task.hip": ["attn_tile.h", "cross_d128_loop.inc", "cross_d64_loop.inc"],
             "cross_f32.hip": ["attn_tile.h", "attn_f32_loop.h"],
             "rotary.hip": ["attn_tile.h"]}
 

@@ -29,251 +29,152 @@
 #include <type_traits>
 
 #include "attn_tile.h"
+#include "cross_tile.h"
 #include "internal.h"
 
 namespace ditango {
 namespace {
 
-__device__ __forceinline__ uint32_t lds_addr(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-
-// s_waitcnt immediate: at most n vector-memory operations outstanding
-constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0F70; }
-
-// Buffer descriptor of raw bytes [base, base + nbytes): loads past the end
-// give zeros and do not access memory.
-__device__ __forceinline__ u32x4 buffer_desc(const void* base, uint32_t nbytes) {
-  const uint64_t p = (uint64_t)(uintptr_t)base;
-  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p),
-               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)) & 0xffffu,
-               (uint32_t)__builtin_amdgcn_readfirstlane(nbytes), 0x00020000u};
-}
-
-// 16-byte direct loads global -> LDS for the wave: lane l's 16 bytes land at
-// LDS byte lds + 16 * l (wave-uniform).  From a descriptor and a byte offset,
-// or from an address.  The waits for them are written out (s_waitcnt vmcnt).
-__device__ __forceinline__ void dma_desc(const u32x4& desc, uint32_t off, uint32_t lds) {
-  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-               :
-               : "v"(off), "s"(desc), "s"(m0v)
-               : "memory", "m0");
-}
-__device__ __forceinline__ void dma_addr(const void* p, uint32_t lds) {
-  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
-               :
-               : "v"(p), "s"(m0v)
-               : "memory", "m0");
-}
-
-template <int D_>
-struct CrossCfg {
-  static constexpr int D = D_, NW = 4, BN = 64, NBUF = 2;
+// One workgroup: NW * 32 rows of one key/value head, one key range.  The waves
+// share the K and V tiles of 64 keys, which land in rings of two tiles by direct
+// loads.
+template <int D_, int NW_>
+struct RowsCfg {
+  static constexpr int D = D_, NW = NW_, BN = 64, NBUF = 2;
   static constexpr int NT = NW * 64, BM = NW * 32;
-  static constexpr int KS = D / 16, KB = BN / 32, DB = D / 32, PS = BN / 16;
+  static constexpr int KS = D / 16, DB = D / 32;
   static constexpr int UNITS = D / 8, ROWB = D * 2, TILEB = BN * ROWB;
   static constexpr int RPL = 1024 / ROWB;          // rows per 1 KiB load
-  static constexpr int LW = TILEB / 1024 / NW;     // loads per wave and tile
+  static constexpr int LOADS = TILEB / 1024;       // 1 KiB loads of a tile
   static constexpr int LDS = 2 * NBUF * TILEB;
-  static_assert(NW * 32 * ROWB <= LDS, "output staging inside the ring");
 };
 
-// One workgroup: 128 rows of one key/value head, one key range.  Four waves of
-// 32 rows share the K and V tiles, which land in a ring of two by direct loads.
-template <int D_, bool LIST>
-__global__ __launch_bounds__(256, 2) void cross_kernel(const CrossArgs a) {
-  using C = CrossCfg<D_>;
+template <class C, int WPE, bool LIST>
+__global__ __launch_bounds__(C::NT, WPE) void cross_kernel(const CrossArgs) {
   constexpr int D = C::D, BN = C::BN;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-
+  Args a = args();
   int t = xcd_remap(blockIdx.x, gridDim.x);
-  const int rt = t % a.row_tiles;
-  t /= a.row_tiles;
-  const int sp = t % a.split;
-  t /= a.split;
-  const int hk = t % a.Hk;
-  const int b = t / a.Hk;
+  const int rt = t % a->row_tiles;
+  t /= a->row_tiles;
+  const int sp = t % a->split;
+  t /= a->split;
+  const int hk = t % a->Hk;
+  const int b = t / a->Hk;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, g = lane >> 5;
 
   // this workgroup's key range: whole tiles
-  const int n = __builtin_amdgcn_readfirstlane(cross_keys(a, b));
-  const int per = ((n + BN - 1) / BN + a.split - 1) / a.split * BN;
+  const int n = __builtin_amdgcn_readfirstlane(live_keys(a, b));
+  const int per = ((n + BN - 1) / BN + a->split - 1) / a->split * BN;
   const int key_begin = min(sp * per, n), key_end = min(key_begin + per, n);
   const int tiles = (key_end - key_begin + BN - 1) / BN;
 
-  const __bf16* kg = (const __bf16*)a.k + b * a.k_batch + hk * a.k_head;
-  const __bf16* vg = (const __bf16*)a.v + b * a.v_batch + hk * a.v_head;
-
   // ---- this lane's query row (rows past the end read the last one and are
   // not stored): B operand, Q[row][16s + 8g .. +8]
-  const int row0 = rt * C::BM + wave * 32;
-  const int row = row0 + lr;
-  const int tok = min(row, a.rows - 1) / a.G, gi = min(row, a.rows - 1) % a.G;
-  const __bf16* qrow = (const __bf16*)a.q + b * a.q_batch + tok * a.q_token + (int64_t)(hk * a.G + gi) * a.q_head;
+  const int row = rt * C::BM + wave * 32 + lr;
   bf16x8 qf[C::KS];
+  {
+    int tok, gi;
+    token_of(a, rt * C::BM, wave * 32 + lr, &tok, &gi);
+    const __bf16* p = (const __bf16*)a->q + b * a->q_batch + tok * a->q_token + (int64_t)(hk * a->G + gi) * a->q_head + 8 * g;
 #pragma unroll
-  for (int s = 0; s < C::KS; ++s) qf[s] = *(const bf16x8*)(qrow + 16 * s + 8 * g);
+    for (int s = 0; s < C::KS; ++s) qf[s] = *(const bf16x8*)(p + 16 * s);
+  }
 
+  const __bf16* kg = (const __bf16*)a->k + b * a->k_batch + hk * a->k_head;
+  const __bf16* vg = (const __bf16*)a->v + b * a->v_batch + hk * a->v_head;
+  const int64_t k_token = a->k_token, v_token = a->v_token;
+  const int32_t* list = LIST ? a->list + (int64_t)b * a->kv_len : nullptr;
+  const __bf16* zeros = (const __bf16*)a->zeros;
+  const float sl2 = a->scale_log2;
+  const uint32_t lds0 = lds_addr(smem);
+  const int ld_row = lane / C::UNITS, ld_unit = lane % C::UNITS;
+  // tile `tile` of K and V into their rings
+  auto load_tile = [&](int tile) {
+    const int key0 = key_begin + tile * BN;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      const uint32_t dst = lds0 + (uint32_t)((which * C::NBUF + tile % C::NBUF) * C::TILEB);
+      const __bf16* base = which ? vg : kg;
+      const int64_t stride = which ? v_token : k_token;
+      u32x4 desc;
+      if constexpr (!LIST)
+        desc = buffer_desc(base + (int64_t)key0 * stride,
+                           (uint32_t)min((int64_t)(key_end - 1 - key0) * stride * 2 + C::ROWB, (int64_t)0x7fffffff));
+#pragma unroll
+      for (int i = 0; i < (C::LOADS + C::NW - 1) / C::NW; ++i) {
+        const int j = wave + i * C::NW;
+        if (C::LOADS % C::NW != 0 && j >= C::LOADS) break;
+        const int r = j * C::RPL + ld_row;
+        const int unit = ld_unit ^ (which ? swz_v<D>(r) : swz_k<D>(r));
+        if constexpr (LIST) {
+          const __bf16* p = zeros;
+          if (key0 + r < key_end) p = base + list[key0 + r] * stride;
+          dma_addr(p + unit * 8, dst + j * 1024);
+        } else {
+          dma_desc(desc, (uint32_t)r * (uint32_t)(stride * 2) + (uint32_t)unit * 16, dst + j * 1024);
+        }
+      }
+    }
+  };
+
+  const FragReader<D> fr(lane);
   f32x16 o[C::DB];
 #pragma unroll
   for (int db = 0; db < C::DB; ++db) o[db] = f32x16{};
   float m = -INFINITY, l = 0.f;
-
-  const uint32_t lds0 = lds_addr(smem);
-  const int ld_row = lane / C::UNITS, ld_unit = lane % C::UNITS;
-  // Tile `tile` of K (which = 0) or V (1) into ring slot tile % 2.
-  auto load_tile = [&](int tile, int which) {
-    const int key0 = key_begin + tile * BN;
-    const uint32_t dst = lds0 + (uint32_t)((which * C::NBUF + tile % C::NBUF) * C::TILEB + wave * C::LW * 1024);
-    const __bf16* base = which ? vg : kg;
-    const int64_t stride = which ? a.v_token : a.k_token;
-    if constexpr (LIST) {
+  if (tiles > 0) load_tile(0);
+#pragma unroll 1
+  for (int i = 0; i < tiles; ++i) {
+    wait_loads();                                    // tile i has landed
+    __syncthreads();
+    if (i + 1 < tiles) load_tile(i + 1);
+    const unsigned char* kt = smem + i % C::NBUF * C::TILEB;
 #pragma unroll
-      for (int i = 0; i < C::LW; ++i) {
-        const int r = (wave * C::LW + i) * C::RPL + ld_row;
-        const int unit = ld_unit ^ (which ? swz_v<D>(r) : swz_k<D>(r));
-        const __bf16* p = (const __bf16*)a.zeros;
-        if (key0 + r < key_end) p = base + a.list[(int64_t)b * a.kv_len + key0 + r] * stride;
-        dma_addr(p + unit * 8, dst + i * 1024);
-      }
-    } else {
-      const int64_t left = key_end > key_begin + tile * BN ? (int64_t)(key_end - 1 - key0) * stride * 2 + C::ROWB : 0;
-      const u32x4 desc = buffer_desc(base + (int64_t)key0 * stride, (uint32_t)min(left, (int64_t)0x7fffffff));
-#pragma unroll
-      for (int i = 0; i < C::LW; ++i) {
-        const int r = (wave * C::LW + i) * C::RPL + ld_row;
-        const int unit = ld_unit ^ (which ? swz_v<D>(r) : swz_k<D>(r));
-        dma_desc(desc, (uint32_t)r * (uint32_t)(stride * 2) + (uint32_t)unit * 16, dst + i * 1024);
-      }
-    }
-  };
-
-  // V^T fragments by transpose reads
-  const int vrow = 4 * g + ((lane & 15) >> 2);
-  const int vdim = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  int voff[C::DB];
-#pragma unroll
-  for (int db = 0; db < C::DB; ++db) {
-    const int dim = 32 * db + vdim;
-    voff[db] = vrow * C::ROWB + ((dim >> 3) ^ swz_v<D>(vrow)) * 16 + (dim & 7) * 2;
-  }
-  auto v_frag = [&](const unsigned char* vs, int s, int db) {
-    const unsigned char* p = vs + 16 * s * C::ROWB + voff[db];
-    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, p)));
-    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, p + 8 * C::ROWB)));
-    return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
-  };
-
-  if (tiles > 0) {
-    load_tile(0, 0);
-    load_tile(0, 1);
-    for (int i = 0; i < tiles; ++i) {
-      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));      // tile i has landed
-      __syncthreads();
-      if (i + 1 < tiles) {
-        load_tile(i + 1, 0);
-        load_tile(i + 1, 1);
-      }
-      const unsigned char* kb = smem + (i % C::NBUF) * C::TILEB;
-      const unsigned char* vb = smem + (C::NBUF + i % C::NBUF) * C::TILEB;
-      f32x16 sc[C::KB];
-#pragma unroll
-      for (int k = 0; k < C::KB; ++k) {
-        sc[k] = f32x16{};
-#pragma unroll
-        for (int s = 0; s < C::KS; ++s)
-          sc[k] = mfma32(*(const bf16x8*)(kb + (k * 32 + lr) * C::ROWB + ((2 * s + g) ^ swz_k<D>(lr)) * 16), qf[s], sc[k]);
-      }
-      if (key_begin + (i + 1) * BN > key_end) {
-#pragma unroll
-        for (int k = 0; k < C::KB; ++k)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (key_begin + i * BN + k * 32 + 8 * (r >> 2) + 4 * g + (r & 3) >= key_end) sc[k][r] = -INFINITY;
-      }
-      float mx = sc[0][0];
-#pragma unroll
-      for (int k = 0; k < C::KB; ++k)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[k][r]);
-      const float mnew = fmaxf(m, pair_max(mx) * a.scale_log2);
-      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mnew);
-      const float mm = mnew == -INFINITY ? 0.f : mnew;
-      m = mnew;
-      l *= alpha;
-#pragma unroll
-      for (int db = 0; db < C::DB; ++db) o[db] *= alpha;
-      bf16x8 pf[C::PS];
-#pragma unroll
-      for (int k = 0; k < C::KB; ++k)
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          f32x8 x;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] = fast_exp2(__builtin_fmaf(sc[k][8 * hh + e], a.scale_log2, -mm));
-            l += x[e];
-          }
-          pf[2 * k + hh] = __builtin_convertvector(x, bf16x8);
-        }
-#pragma unroll
-      for (int s = 0; s < C::PS; ++s)
-#pragma unroll
-        for (int db = 0; db < C::DB; ++db) o[db] = mfma32(v_frag(vb, s, db), pf[s], o[db]);
+    for (int st = 0; st < 2; ++st) {
+      const int key = key_begin + i * BN + st * 32;
+      if (st > 0 && key >= key_end) break;
+      f32x16 sc = fr.scores(kt + st * 32 * C::ROWB, qf);
+      if (key + 32 > key_end) mask_keys(sc, key_end - key, g);
+      bf16x8 pf[2];
+      softmax_step<C::DB>(sc, pf, o, m, l, sl2, i + st == 0);
+      fr.template values<false>(kt + C::NBUF * C::TILEB + st * 32 * C::ROWB, pf, o);
     }
   }
-  __syncthreads();                                   // the ring is free
 
-  // ---- epilogue
+  // ---- the rows' state (two lanes' quarters of 16 dims make 32 bytes)
+  a = args();
   const float lt = pair_sum(l);
   const float inv = lt > 0.f ? 1.0f / lt : 0.f;
   const float lse = lt > 0.f ? (m + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
-  const bool ok = row < a.rows;
-  const int h = hk * a.G + gi;
-  if (a.split > 1) {
-    const int64_t at = (((int64_t)sp * a.B + b) * a.H + h) * a.q_len + tok;
-    if (ok) {
-      float* dst = a.part_out + at * D + 4 * g;
+  if (row >= a->rows) return;
+  int tok, gi;
+  token_of(a, rt * C::BM, wave * 32 + lr, &tok, &gi);
+  const int h = hk * a->G + gi;
+  const int64_t at = ((int64_t)b * a->H + h) * a->q_len + tok;
+  if (a->split > 1) {
+    const int64_t ap = (int64_t)sp * a->B * a->H * a->q_len + at;
+    float* dst = a->part_out + ap * D + 4 * g;
 #pragma unroll
-      for (int db = 0; db < C::DB; ++db)
+    for (int db = 0; db < C::DB; ++db)
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          f32x4 x;
+      for (int r4 = 0; r4 < 4; ++r4) {
+        f32x4 x;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = o[db][4 * r4 + e] * inv;
-          *(f32x4*)(dst + db * 32 + 8 * r4) = x;
-        }
-      if (g == 0) a.part_lse[at] = lse;
-    }
-    return;
-  }
-  if (ok && g == 0 && a.lse != nullptr) a.lse[((int64_t)b * a.H + h) * a.q_len + tok] = lse;
-  // rows through LDS (16-byte units swizzled by row), then stored whole
-  unsigned char* stage = smem + wave * 32 * C::ROWB;
+        for (int e = 0; e < 4; ++e) x[e] = o[db][4 * r4 + e] * inv;
+        *(f32x4*)(dst + db * 32 + 8 * r4) = x;
+      }
+    if (g == 0) a->part_lse[ap] = lse;
+  } else {
+    __bf16* dst = (__bf16*)a->out + (((int64_t)b * a->q_len + tok) * a->H + h) * D + 8 * g;
 #pragma unroll
-  for (int db = 0; db < C::DB; ++db)
+    for (int db = 0; db < C::DB; ++db)
 #pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      f32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = o[db][4 * r4 + e] * inv;
-      const int unit = (4 * db + r4) ^ (lr & (C::UNITS - 1));
-      *(bf16x4*)(stage + lr * C::ROWB + unit * 16 + 8 * g) = __builtin_convertvector(x, bf16x4);
-    }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 32 / C::RPL; ++i) {
-    const int r = i * C::RPL + ld_row;
-    if (row0 + r < a.rows) {
-      const int rtok = (row0 + r) / a.G, rh = hk * a.G + (row0 + r) % a.G;
-      *(bf16x8*)((__bf16*)a.out + (((int64_t)b * a.q_len + rtok) * a.H + rh) * D + ld_unit * 8) =
-          *(const bf16x8*)(stage + r * C::ROWB + (ld_unit ^ (r & (C::UNITS - 1))) * 16);
-    }
+      for (int half = 0; half < 2; ++half) *(bf16x8*)(dst + 32 * db + 16 * half) = row_units(o[db], half, inv);
+    if (g == 0 && a->lse != nullptr) a->lse[at] = lse;
   }
 }
 
@@ -306,32 +207,96 @@ __global__ __launch_bounds__(1024) void cross_list_kernel(const CrossArgs a) {
   if (b == 0 && tid < 128) a.zeros[tid] = 0.f;
 }
 
+// The rows of the live keys of every sequence, one after another, for a kernel
+// whose tile loads take rows at a fixed distance.  A workgroup moves the rows
+// of kPackKeys keys; where they go follows from the mask in front of them,
+// which it counts by itself.
+constexpr int kPackKeys = 16;
+__global__ __launch_bounds__(256) void cross_pack_kernel(const CrossArgs a, int units) {
+  __shared__ int sums[4];
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  const int k0 = blockIdx.x * kPackKeys;
+  const int n = a.lens == nullptr ? a.kv_len : min(max(a.lens[b], 0), a.kv_len);
+  const uint8_t* mask = a.mask + (int64_t)b * a.kv_len;
+  int before = 0;
+  for (int k = tid; k < min(k0, n); k += 256) before += mask[k] != 0;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) before += __shfl_xor(before, d, 64);
+  if (lane == 0) sums[tid >> 6] = before;
+  __syncthreads();
+  int to = sums[0] + sums[1] + sums[2] + sums[3];
+  for (int k = k0; k < min(k0 + kPackKeys, n); ++k) {
+    if (mask[k] == 0) continue;
+    const int64_t dst = ((int64_t)b * a.kv_len + to) * a.Hk * units;
+    for (int i = tid; i < 2 * a.Hk * units; i += 256) {
+      const bool v = i >= a.Hk * units;
+      const int u = v ? i - a.Hk * units : i;
+      const int64_t src = v ? b * a.v_batch + k * a.v_token + u / units * a.v_head
+                            : b * a.k_batch + k * a.k_token + u / units * a.k_head;
+      ((u32x4*)(v ? a.packed_v : a.packed_k))[dst + u] =
+          *(const u32x4*)((const __bf16*)(v ? a.v : a.k) + src + u % units * 8);
+    }
+    ++to;
+  }
+  // the workgroup of the last keys has seen them all
+  if (tid == 0 && blockIdx.x == gridDim.x - 1) a.count[b] = to;
+}
+
 // Composes the partial states of a split launch: a wave per row, in the order
-// of the key ranges.
+// of the key ranges.  Bound by latency: lane p holds range p's weight (64
+// ranges at a time), and the ranges' rows are loaded in batches.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
-  constexpr int E = D / 64;
+  constexpr int E = D / 64, kBatch = 8;
+  typedef float VE __attribute__((ext_vector_type(E)));
   const int64_t rows = (int64_t)a.B * a.H * a.q_len;
   const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (r >= rows) return;
   const int lane = threadIdx.x & 63;
+  const int b = (int)(r / a.q_len / a.H);
+  // ranges of fixed length behind the sequence's end have not been written
+  const int parts = a.chunk > 0 ? min(a.split, (cross_keys(a, b) + a.chunk - 1) / a.chunk) : a.split;
   float mx = -INFINITY;
   bool bad = false;
-  for (int p = 0; p < a.split; ++p) {
+  for (int p = lane; p < parts; p += 64) {
     const float x = a.part_lse[p * rows + r];
     bad |= x != x;
     mx = fmaxf(mx, x);
   }
-  const float mm = mx == -INFINITY ? 0.f : mx;
-  float tot = 0.f, acc[E] = {};
-  for (int p = 0; p < a.split; ++p) {
-    const float w = fast_exp2((a.part_lse[p * rows + r] - mm) * 1.4426950408889634f);
-    tot += w;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(w, a.part_out[(p * rows + r) * D + lane * E + e], acc[e]);
+  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+  bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+  const float mm = mx == -INFINITY ? 0.f : mx;
+  float tot = 0.f;
+  VE acc;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const float mine = p0 + lane < parts ? a.part_lse[(p0 + lane) * rows + r] : -INFINITY;
+    const float w = fast_exp2((mine - mm) * 1.4426950408889634f);
+    float sum = w;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+    tot += sum;
+    const int np = min(parts - p0, 64);
+    for (int q0 = 0; q0 < np; q0 += kBatch) {
+      VE x[kBatch];
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q)
+        x[q] = *(const VE*)(a.part_out + ((p0 + min(q0 + q, np - 1)) * rows + r) * D + lane * E);
+#pragma unroll
+      for (int q = 0; q < kBatch; ++q) {
+        // (past the last range the weight is left out, not 0 times a value)
+        if (q0 + q < np) {
+          const float wq = __shfl(w, q0 + q, 64);
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(wq, x[q][e], acc[e]);
+        }
+      }
+    }
   }
   const float inv = tot > 0.f ? 1.0f / tot : bad ? NAN : 0.f;
-  const int64_t tok = r % a.q_len, h = r / a.q_len % a.H, b = r / a.q_len / a.H;
+  const int64_t tok = r % a.q_len, h = r / a.q_len % a.H;
   T* dst = (T*)a.out + ((b * a.q_len + tok) * a.H + h) * D + lane * E;
 #pragma unroll
   for (int e = 0; e < E; ++e) dst[e] = (T)(acc[e] * inv);
@@ -339,39 +304,129 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
     a.lse[r] = tot > 0.f ? mx + __builtin_amdgcn_logf(tot) * kLn2 : bad ? NAN : -INFINITY;
 }
 
-template <int D, bool LIST>
-hipError_t launch_rows(const CrossArgs& a0, hipStream_t s) {
-  using C = CrossCfg<D>;
+template <class C, int WPE, bool LIST>
+hipError_t launch_rows_cfg(const CrossArgs& a0, hipStream_t s) {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  e = set_kernel_lds<&cross_kernel<D, LIST>, C::LDS>(dev);
+  e = set_kernel_lds<&cross_kernel<C, WPE, LIST>, C::LDS>(dev);
   if (e != hipSuccess) return e;
   CrossArgs a = a0;
   a.row_tiles = (a.rows + C::BM - 1) / C::BM;
   const int64_t grid = (int64_t)a.row_tiles * a.split * a.Hk * a.B;
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((cross_kernel<D, LIST>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);
+  hipLaunchKernelGGL((cross_kernel<C, WPE, LIST>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);
   return hipGetLastError();
+}
+template <int D, bool LIST>
+hipError_t launch_rows(const CrossArgs& a, hipStream_t s) {
+#ifdef SWEEP
+  const int cfg = getenv("RES") ? atoi(getenv("RES")) : 0;
+  if constexpr (!LIST) {
+  if (D == 64 && cfg == 1) return launch_rows_cfg<RowsCfg<D, 4>, 4, LIST>(a, s);
+  if (cfg == 2) return launch_rows_cfg<RowsCfg<D, 4>, 3, LIST>(a, s);
+  }
+#endif
+  return launch_rows_cfg<RowsCfg<D, 4>, 2, LIST>(a, s);
+}
+
+// Estimated times in us of a launch of the two kernels that share a head's keys
+// between many rows, by how their workgroups fill the compute units, with the
+// split of the keys that is best for each (its join takes 4 us).  Measured (one
+// card): kRows a tile of 64 keys 1.4 us (D=64 0.9) where a compute unit has one
+// workgroup, 1.04 (0.53) for each where it has more, and 2.7 (1.3) beside them;
+// kTask 1.13 (0.97) a tile and 6.5 (4.9) a task.
+struct Estimate {
+  double us;
+  int split;
+};
+Estimate estimate_rows(int64_t workgroups, int64_t tiles, int D, int cus) {
+  const double one = D == 128 ? 1.4 : 0.9, each = D == 128 ? 1.04 : 0.53, beside = D == 128 ? 2.7 : 1.3;
+  Estimate best{1e30, 1};
+  for (int64_t s = 1; s == 1 || (s <= tiles / 2 && s <= 64); ++s) {
+    const double n = (double)(workgroups * s) / cus, w = n > 2 ? n : n > 1 ? 2 : 1;
+    const double tile = w * each > one ? w * each : one;
+    const double us = (double)((tiles + s - 1) / s) * tile + (w * beside > 2 ? w * beside : 2) + (s > 1 ? 4 : 0);
+    if (us < best.us) best = {us, (int)s};
+  }
+  return best;
+}
+Estimate estimate_task(int64_t tasks, int64_t tiles, int D, int cus) {
+  const double tile = D == 128 ? 1.13 : 0.97, beside = D == 128 ? 6.5 : 4.9;
+  Estimate best{1e30, 1};
+  for (int64_t s = 1; s == 1 || (s <= tiles / 8 && s <= 16); ++s) {
+    const double rounds = (double)((tasks * s + cus - 1) / cus);
+    const double us = rounds * ((double)((tiles + s - 1) / s) * tile + beside) + (s > 1 ? 4 : 0);
+    if (us < best.us) best = {us, (int)s};
+  }
+  return best;
+}
+
+// The kernel a bf16 call runs, and its split.
+//  - kFew for up to 32 rows of a key/value head: 8 x 24 heads, 8 of them with
+//    keys, of one token against 16,384 keys 103 us (kRows 111), 12 heads against
+//    77 keys 4.7 us (5.4).
+//  - kResident where the keys fit LDS and every wave has two blocks of rows at
+//    least: 9,450 rows x 40 heads against 256 keys 65 us (kRows 78, kTask 83),
+//    14,850 x 48 at D=64 against 512 112 us (117, 137); but 2 x 4,095 x 12
+//    against 256 30 us (kRows 25).
+//  - kTask or kRows as estimated: 9,450 x 40 against 512 keys 112 us (kRows 119),
+//    against 1,024 178 us (210); 700 x 24 against 512 20 us (16).
+void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
+  const int64_t heads = (int64_t)a.Hk * a.B, rows = a.rows, tiles = (a.kv_len + 63) / 64;
+  if (rows <= 32) {
+    p->form = CrossPlan::kFew;
+    if (a.kv_len > 768) {
+      // four workgroups for a compute unit, of 256 keys at least (the join
+      // takes as long as 600 keys)
+      const int64_t want = (4 * (int64_t)cus + heads - 1) / heads;
+      const int64_t chunk = ((a.kv_len + want - 1) / want + 127) / 128 * 128;
+      p->chunk = (int)(chunk > 256 ? chunk : 256);
+      p->split = (a.kv_len + p->chunk - 1) / p->chunk;
+    } else {
+      p->chunk = a.kv_len;
+    }
+    return;
+  }
+  if (a.kv_len <= cross_resident_keys(D) && (rows + 31) / 32 * heads >= 24 * (int64_t)cus) {
+    p->form = CrossPlan::kResident;
+    return;
+  }
+  const Estimate r = estimate_rows((rows + 127) / 128 * heads, tiles, D, cus);
+  p->split = r.split;
+  CrossArgs t = a;
+  if (a.mask != nullptr) t.k_token = t.v_token = (int64_t)a.Hk * D;     // as packed
+  if (!cross_task_fits(t, D)) return;
+  Estimate k = estimate_task((rows + 255) / 256 * heads, tiles, D, cus);
+  if (k.us < r.us) {
+    p->form = CrossPlan::kTask;
+    p->split = k.split;
+  }
 }
 
 }  // namespace
 
 hipError_t plan_cross(const CrossArgs& a, ditango_dtype dt, int D, CrossPlan* p) {
-  *p = CrossPlan{1, 0};
+  *p = CrossPlan{CrossPlan::kRows, 1, 0, 0, 0};
   int dev = 0, cus = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return e;
-  const int bm = dt == DITANGO_BF16 ? 128 : cross_f32_rows(D);
-  const int64_t groups = (int64_t)((a.rows + bm - 1) / bm) * a.Hk * a.B;
-  // a launch that leaves compute units idle splits its keys: two tiles at
-  // least in each range
-  const int64_t tiles = (a.kv_len + 63) / 64;
-  int64_t split = (2 * (int64_t)cus + groups - 1) / groups;
-  split = split < tiles / 2 ? split : tiles / 2;
-  p->split = split > 1 ? (int)split : 1;
-  p->bytes = cross_list_bytes(a);
+  const size_t keys = (size_t)a.B * a.kv_len;
+  if (dt == DITANGO_BF16) {
+    choose_form(a, D, cus, p);
+  } else {
+    // a launch that leaves half the compute units idle splits its keys, two
+    // tiles at least in each range
+    const int bm = cross_f32_rows(D);
+    const int64_t groups = (int64_t)((a.rows + bm - 1) / bm) * a.Hk * a.B, tiles = (a.kv_len + 63) / 64;
+    const int64_t split = 2 * groups <= cus ? 2 * (int64_t)cus / groups : 1;
+    p->split = (int)(split < tiles / 2 ? split : tiles / 2 > 1 ? tiles / 2 : 1);
+  }
+  if (a.mask != nullptr)
+    p->need = align_up256((size_t)a.B * 4) +
+              (p->form == CrossPlan::kTask ? 2 * align_up256(keys * a.Hk * D * 2) : align_up256(keys * 4) + 512);
+  p->bytes = p->need;
   if (p->split > 1) {
     const size_t rows = (size_t)a.B * a.H * a.q_len;
     p->bytes += align_up256(p->split * rows * D * 4) + align_up256(p->split * rows * 4);
@@ -379,28 +434,53 @@ hipError_t plan_cross(const CrossArgs& a, ditango_dtype dt, int D, CrossPlan* p)
   return hipSuccess;
 }
 
-hipError_t launch_cross(const CrossArgs& a0, ditango_dtype dt, int D, void* ws, size_t ws_bytes, hipStream_t s) {
-  CrossPlan p;
-  hipError_t e = plan_cross(a0, dt, D, &p);
-  if (e != hipSuccess) return e;
+hipError_t launch_cross(const CrossArgs& a0, const CrossPlan& p, ditango_dtype dt, int D, void* ws, size_t ws_bytes,
+                        hipStream_t s) {
   CrossArgs a = a0;
+  hipError_t e = hipSuccess;
   char* w = (char*)ws;
+  const size_t keys = (size_t)a.B * a.kv_len;
   if (a.mask != nullptr) {
-    a.list = (int32_t*)w;
-    a.count = (int32_t*)(w + align_up256((size_t)a.B * a.kv_len * 4));
-    a.zeros = (float*)((char*)a.count + align_up256((size_t)a.B * 4));
-    hipLaunchKernelGGL(cross_list_kernel, dim3(a.B), dim3(1024), 0, s, a);
+    a.count = (int32_t*)w;
+    char* at = w + align_up256((size_t)a.B * 4);
+    if (p.form == CrossPlan::kTask) {
+      a.packed_k = at;
+      a.packed_v = at + align_up256(keys * a.Hk * D * 2);
+      const dim3 grid((unsigned)((a.kv_len + kPackKeys - 1) / kPackKeys), (unsigned)a.B);
+      hipLaunchKernelGGL(cross_pack_kernel, grid, dim3(256), 0, s, a, D / 8);
+      // what follows sees the live keys as a prefix of dense rows
+      a.k = a.packed_k;
+      a.v = a.packed_v;
+      a.k_head = a.v_head = D;
+      a.k_token = a.v_token = (int64_t)a.Hk * D;
+      a.k_batch = a.v_batch = a.kv_len * a.k_token;
+      a.lens = a.count;
+      a.mask = nullptr;
+    } else {
+      a.list = (int32_t*)at;
+      a.zeros = (float*)(at + align_up256(keys * 4));
+      hipLaunchKernelGGL(cross_list_kernel, dim3(a.B), dim3(1024), 0, s, a);
+    }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  // (one chunk, of all keys, without room for the partial states)
   a.split = 1;
+  a.chunk = p.chunk > 0 ? a.kv_len : 0;
   const size_t rows = (size_t)a.B * a.H * a.q_len;
   if (p.split > 1 && ws_bytes >= p.bytes) {
     a.split = p.split;
-    a.part_out = (float*)(w + cross_list_bytes(a));
+    a.chunk = p.chunk;
+    a.part_out = (float*)(w + p.need);
     a.part_lse = (float*)((char*)a.part_out + align_up256(p.split * rows * D * 4));
   }
-  if (dt == DITANGO_F32)
+  if (p.form == CrossPlan::kTask)
+    e = launch_cross_task(a, D, s);
+  else if (p.form == CrossPlan::kResident)
+    e = launch_cross_resident(a, D, s);
+  else if (p.form == CrossPlan::kFew)
+    e = launch_cross_few(a, D, s);
+  else if (dt == DITANGO_F32)
     e = launch_cross_f32(a, D, s);
   else if (D == 128)
     e = a.mask ? launch_rows<128, true>(a, s) : launch_rows<128, false>(a, s);

@@ -1,0 +1,173 @@
+// cross_resident.hip - the cross attention of many query rows to few keys,
+// bf16 (gfx950): the keys and values of a head stay in LDS.
+//
+// A prompt's states of one head are small: 256 keys at D=64 take 64 KB.  A
+// workgroup of eight waves, one per compute unit, loads them once and its waves
+// walk over blocks of query rows by themselves, without a barrier: while one
+// wave of a SIMD takes exponentials the other's products run.  The next
+// block's queries are on their way from the last use of this one's on.
+#include <stdlib.h>
+#include <type_traits>
+
+#include "attn_tile.h"
+#include "cross_tile.h"
+#include "internal.h"
+
+namespace ditango {
+namespace {
+
+template <int D_, int NW_>
+struct ResidentCfg {
+  static constexpr int D = D_, NW = NW_, BN = 64;
+  static constexpr int NT = NW * 64, BM = 32;
+  static constexpr int KS = D / 16, DB = D / 32;
+  static constexpr int UNITS = D / 8, ROWB = D * 2, TILEB = BN * ROWB;
+  static constexpr int RPL = 1024 / ROWB;
+  static constexpr int LOADS = TILEB / 1024;       // 1 KiB loads of a tile
+  static constexpr int MAX_TILES = 163840 / (2 * TILEB);
+  static constexpr int LDS = MAX_TILES * 2 * TILEB;
+};
+
+template <class C, bool LIST>
+__global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const CrossArgs) {
+  constexpr int D = C::D, BN = C::BN;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, g = lane >> 5;
+  const uint32_t lds0 = lds_addr(smem);
+
+  // this workgroup's blocks of rows: a contiguous share, of one head or a few
+  Args a = args();
+  const int groups = a->Hk * a->B;
+  const int64_t all = (int64_t)a->row_tiles * groups;
+  const int w = xcd_remap(blockIdx.x, gridDim.x);
+  int64_t at = all * w / gridDim.x;
+  const int64_t end = all * (w + 1) / gridDim.x;
+
+  const int ld_row = lane / C::UNITS, ld_unit = lane % C::UNITS;
+  const FragReader<D> fr(lane);
+  bf16x8 qf[C::KS];
+  while (at < end) {
+    a = args();
+    const int grp = (int)(at / a->row_tiles);
+    const int hk = grp / a->B, b = grp % a->B;
+    const int first = (int)(at - (int64_t)grp * a->row_tiles);
+    const int last = (int)min((int64_t)a->row_tiles, first + (end - at));   // row blocks [first, last)
+    at += last - first;
+    const int n = __builtin_amdgcn_readfirstlane(live_keys(a, b));
+    const int tiles = (n + BN - 1) / BN, steps = (n + 31) / 32;
+    const float sl2 = a->scale_log2;
+
+    // ---- K and V of the head: tile i of K, then of V
+    __syncthreads();                                    // the head before is done with
+    const __bf16* kg = (const __bf16*)a->k + b * a->k_batch + hk * a->k_head;
+    const __bf16* vg = (const __bf16*)a->v + b * a->v_batch + hk * a->v_head;
+    for (int u = wave; u < tiles * 2 * C::LOADS; u += C::NW) {
+      const int i = u / (2 * C::LOADS), which = u / C::LOADS % 2, j = u % C::LOADS;
+      const __bf16* base = which ? vg : kg;
+      const int64_t stride = which ? a->v_token : a->k_token;
+      const uint32_t dst = lds0 + (uint32_t)((2 * i + which) * C::TILEB + j * 1024);
+      const int r = j * C::RPL + ld_row;
+      const int unit = ld_unit ^ (which ? swz_v<D>(r) : swz_k<D>(r));
+      if constexpr (LIST) {
+        const __bf16* p = (const __bf16*)a->zeros;
+        if (i * BN + r < n) p = base + a->list[(int64_t)b * a->kv_len + i * BN + r] * stride;
+        dma_addr(p + unit * 8, dst);
+      } else {
+        const u32x4 desc = buffer_desc(base + (int64_t)i * BN * stride,
+                                       (uint32_t)min((int64_t)(n - 1 - i * BN) * stride * 2 + C::ROWB, (int64_t)0x7fffffff));
+        dma_desc(desc, (uint32_t)r * (uint32_t)(stride * 2) + (uint32_t)unit * 16, dst);
+      }
+    }
+    auto load_queries = [&](int blk) {
+      a = args();
+      int tok, gi;
+      token_of(a, blk * 32, lr, &tok, &gi);
+      const __bf16* p = (const __bf16*)a->q + b * a->q_batch + tok * a->q_token + (int64_t)(hk * a->G + gi) * a->q_head + 8 * g;
+#pragma unroll
+      for (int s = 0; s < C::KS; ++s) qf[s] = *(const bf16x8*)(p + 16 * s);
+    };
+    if (first + wave < last) load_queries(first + wave);
+    wait_loads();
+    __syncthreads();
+    for (int u = wave; u < tiles * 4; u += C::NW) fr.order_values(smem + (u / 4 * 2 + 1) * C::TILEB, u % 4);
+    __syncthreads();
+
+    for (int blk = first + wave; blk < last; blk += C::NW) {
+      f32x16 o[C::DB];
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db) o[db] = f32x16{};
+#pragma unroll 1
+      for (int i = 0; i < steps; ++i) {
+        const unsigned char* kt = smem + i / 2 * 2 * C::TILEB + i % 2 * 32 * C::ROWB;
+        f32x16 sc = fr.scores(kt, qf);
+        if (i + 1 == steps) {
+          load_queries(blk + C::NW < last ? blk + C::NW : blk);
+          if ((i + 1) * 32 > n) mask_keys(sc, n - i * 32, g);
+        }
+        bf16x8 pf[2];
+        softmax_step<C::DB>(sc, pf, o, m, l, sl2, i == 0);
+        fr.template values<true>(kt + C::TILEB, pf, o);
+      }
+      if (steps == 0) load_queries(blk + C::NW < last ? blk + C::NW : blk);
+
+      a = args();
+      // ---- the rows' state: two lanes' quarters of 16 dims make rows of 32 bytes
+      const float lt = pair_sum(l);
+      const float inv = lt > 0.f ? 1.0f / lt : 0.f;
+      const int row = blk * 32 + lr;
+      if (row < a->rows) {
+        int tok, gi;
+        token_of(a, blk * 32, lr, &tok, &gi);
+        const int h = hk * a->G + gi;
+        if (g == 0 && a->lse != nullptr)
+          a->lse[((int64_t)b * a->H + h) * a->q_len + tok] =
+              lt > 0.f ? (m + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
+        __bf16* dst = (__bf16*)a->out + (((int64_t)b * a->q_len + tok) * a->H + h) * D + 8 * g;
+#pragma unroll
+        for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) *(bf16x8*)(dst + 32 * db + 16 * half) = row_units(o[db], half, inv);
+      }
+    }
+  }
+}
+
+template <class C, bool LIST>
+hipError_t launch_resident(const CrossArgs& a0, int cus, int dev, hipStream_t s) {
+  const hipError_t e = set_kernel_lds<&cross_resident_kernel<C, LIST>, C::LDS>(dev);
+  if (e != hipSuccess) return e;
+  CrossArgs a = a0;
+  a.row_tiles = (a.rows + C::BM - 1) / C::BM;
+  const int64_t all = (int64_t)a.row_tiles * a.Hk * a.B;
+  const int64_t want = (all + C::NW - 1) / C::NW;
+  const int grid = (int)(want < cus ? want : cus);
+  const size_t lds = (size_t)(a.kv_len + C::BN - 1) / C::BN * 2 * C::TILEB;
+  hipLaunchKernelGGL((cross_resident_kernel<C, LIST>), dim3((unsigned)grid), dim3(C::NT), lds, s, a);
+  return hipGetLastError();
+}
+
+using Resident128 = ResidentCfg<128, 12>;
+using Resident64 = ResidentCfg<64, 16>;
+
+}  // namespace
+
+int cross_resident_keys(int D) { return (D == 128 ? Resident128::MAX_TILES : Resident64::MAX_TILES) * 64; }
+
+hipError_t launch_cross_resident(const CrossArgs& a, int D, hipStream_t s) {
+  int dev = 0, cus = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) return e;
+#ifdef SWEEP
+  const int cfg = getenv("RES") ? atoi(getenv("RES")) : 0;
+  if (D == 128 && cfg == 1) return launch_resident<ResidentCfg<128, 8>, false>(a, cus, dev, s);
+  if (D == 64 && cfg == 1) return launch_resident<ResidentCfg<64, 12>, false>(a, cus, dev, s);
+#endif
+  if (D == 128) return a.mask ? launch_resident<Resident128, true>(a, cus, dev, s) : launch_resident<Resident128, false>(a, cus, dev, s);
+  return a.mask ? launch_resident<Resident64, true>(a, cus, dev, s) : launch_resident<Resident64, false>(a, cus, dev, s);
+}
+
+}  // namespace ditango

@@ -1,0 +1,206 @@
+// cross_tile.h - tile loads and the steps over one key tile that the bf16
+// kernels of the cross attention share.
+#pragma once
+
+#include "attn_tile.h"
+#include "internal.h"
+
+namespace ditango {
+namespace {
+
+__device__ __forceinline__ uint32_t lds_addr(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+// The kernel's arguments, as if read for the first time: what a long loop does
+// not use stays out of its scalar registers.
+typedef const __attribute__((address_space(4))) CrossArgs* Args;
+__device__ __forceinline__ Args args() {
+  Args p = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return p;
+}
+// Live keys of sequence b.
+__device__ __forceinline__ int live_keys(Args a, int b) {
+  if (a->mask != nullptr) return a->count[b];
+  return a->lens == nullptr ? a->kv_len : min(max(a->lens[b], 0), a->kv_len);
+}
+
+// Token and head (of the G that share a key/value head) of row row0 + r; rows
+// past the end give the last one's.  row0 is wave-uniform.
+__device__ __forceinline__ void token_of(Args a, int row0, int r, int* tok, int* gi) {
+  const int row = min(row0 + r, a->rows - 1);
+  if (a->G == 1) {
+    *tok = row;
+    *gi = 0;
+  } else {
+    const int tok0 = row0 / a->G;
+    const uint32_t x = (uint32_t)(row - tok0 * a->G);     // below 256 + G: the product is exact
+    const uint32_t y = __umulhi(x, a->g_inverse);
+    *tok = tok0 + (int)y;
+    *gi = (int)(x - y * (uint32_t)a->G);
+  }
+}
+
+// s_waitcnt immediate: at most n vector-memory operations outstanding
+constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0F70; }
+
+// this wave's loads, into registers and into LDS, have landed
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Buffer descriptor of raw bytes [base, base + nbytes): loads past the end
+// give zeros and do not access memory.
+__device__ __forceinline__ u32x4 buffer_desc(const void* base, uint32_t nbytes) {
+  const uint64_t p = (uint64_t)(uintptr_t)base;
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)p),
+               (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(p >> 32)) & 0xffffu,
+               (uint32_t)__builtin_amdgcn_readfirstlane(nbytes), 0x00020000u};
+}
+
+// 16-byte direct loads global -> LDS for the wave: lane l's 16 bytes land at
+// LDS byte lds + 16 * l (wave-uniform).  From a descriptor and a byte offset,
+// or from an address.  The waits for them are written out.
+__device__ __forceinline__ void dma_desc(const u32x4& desc, uint32_t off, uint32_t lds) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+               :
+               : "v"(off), "s"(desc), "s"(m0v)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void dma_addr(const void* p, uint32_t lds) {
+  const uint32_t m0v = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(p), "s"(m0v)
+               : "memory", "m0");
+}
+
+// Fragments of a 64-key tile in LDS (rows of D elements, 16-byte units
+// swizzled as attn_tile.h says) and the products with them.
+template <int D>
+struct FragReader {
+  static constexpr int KS = D / 16, DB = D / 32, ROWB = D * 2;
+  int lane, kswz, voff[DB];
+  __device__ __forceinline__ explicit FragReader(int lane_) : lane(lane_) {
+    const int g = lane >> 5;
+    kswz = swz_k<D>(lane & 31);
+    // V^T by transpose reads: source lane r of a 16-lane group points at row
+    // 4g + r/4 (+ 16s + 8) and dims 32db + 16*(group%2) + 4*(r%4)
+    const int vrow = 4 * g + ((lane & 15) >> 2);
+    const int vdim = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const int dim = 32 * db + vdim;
+      voff[db] = vrow * ROWB + ((dim >> 3) ^ swz_v<D>(vrow)) * 16 + (dim & 7) * 2;
+    }
+  }
+  __device__ __forceinline__ bf16x8 key_frag(const unsigned char* kt, int kb, int s) const {
+    return *(const bf16x8*)(kt + (kb * 32 + (lane & 31)) * ROWB + ((2 * s + (lane >> 5)) ^ kswz) * 16);
+  }
+  __device__ __forceinline__ bf16x8 value_frag(const unsigned char* vt, int s, int db) const {
+    const unsigned char* p = vt + 16 * s * ROWB + voff[db];
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, p)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, p + 8 * ROWB)));
+    return __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], hi[0], hi[1]});
+  }
+  // The same fragment where the tile's V lies as fragments, one after another:
+  // one read instead of two.
+  __device__ __forceinline__ bf16x8 ordered_frag(const unsigned char* vt, int s, int db) const {
+    return *(const bf16x8*)(vt + 16 * s * ROWB + db * 1024 + lane * 16);
+  }
+  // Rows 16s ... 16s + 15 of V -> the fragments of its DB blocks of dims, in place.
+  __device__ __forceinline__ void order_values(unsigned char* vt, int s) const {
+    bf16x8 x[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db) x[db] = value_frag(vt, s, db);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *(bf16x8*)(vt + 16 * s * ROWB + db * 1024 + lane * 16) = x[db];
+  }
+  // S^T = K Q^T of 32 keys
+  __device__ __forceinline__ f32x16 scores(const unsigned char* kt, const bf16x8 (&qf)[KS]) const {
+    f32x16 sc = f32x16{};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sc = mfma32(key_frag(kt, 0, s), qf[s], sc);
+    return sc;
+  }
+  // O^T += V^T P^T of 32 keys
+  template <bool ORDERED>
+  __device__ __forceinline__ void values(const unsigned char* vt, const bf16x8 (&pf)[2], f32x16 (&o)[DB]) const {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        o[db] = mfma32(ORDERED ? ordered_frag(vt, s, db) : value_frag(vt, s, db), pf[s], o[db]);
+  }
+};
+
+// keys at or past `left` of the step -> -inf
+__device__ __forceinline__ void mask_keys(f32x16& sc, int left, int g) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (8 * (r >> 2) + 4 * g + (r & 3) >= left) sc[r] = -INFINITY;
+}
+
+// Scores of 32 keys -> probabilities against the running maximum m, row sum l
+// (this lane's keys).  m is the first step's maximum, and raised only where a
+// lane's sum over a step then passes 2^40 or is not a number: below that
+// float32 holds the sums, and the result does not depend on which m was used.
+template <int DB>
+__device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], f32x16 (&o)[DB], float& m, float& l,
+                                             float sl2, bool first) {
+  float sum;
+  auto raise = [&] {
+    float mx = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    const float mnew = fmaxf(m, pair_max(mx) * sl2);
+    if (!first) {
+      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mnew);
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= alpha;
+    }
+    m = mnew;
+  };
+  auto probs = [&] {
+    const float mm = m == -INFINITY ? 0.f : m;
+    sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x8 x;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[e] = fast_exp2(__builtin_fmaf(sc[8 * h + e], sl2, -mm));
+        sum += x[e];
+      }
+      pf[h] = __builtin_convertvector(x, bf16x8);
+    }
+  };
+  if (first) raise();
+  probs();
+  if (!first && __builtin_amdgcn_ballot_w64(!(sum <= 0x1p40f)) != 0) {
+    raise();
+    probs();
+  }
+  l += sum;
+}
+
+// Unit `half` of a lane's row in a 32-dim block of the accumulators, times
+// `x`: lanes l and l ^ 32 hold dims 8r + 4g ... + 3 (r = 0 ... 3) of row
+// l % 32; here lane l gets dims 16 * half + 8g ... + 7.
+__device__ __forceinline__ bf16x8 row_units(const f32x16& o, int half, float x) {
+  f32x4 a, b;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    a[e] = o[8 * half + e] * x;
+    b[e] = o[8 * half + 4 + e] * x;
+  }
+  const u32x2 pa = __builtin_bit_cast(u32x2, __builtin_convertvector(a, bf16x4));
+  const u32x2 pb = __builtin_bit_cast(u32x2, __builtin_convertvector(b, bf16x4));
+  const auto r0 = __builtin_amdgcn_permlane32_swap(pa[0], pb[0], false, false);
+  const auto r1 = __builtin_amdgcn_permlane32_swap(pa[1], pb[1], false, false);
+  return __builtin_bit_cast(bf16x8, u32x4{r0[0], r1[0], r0[1], r1[1]});
+}
+
+}  // namespace
+}  // namespace ditango

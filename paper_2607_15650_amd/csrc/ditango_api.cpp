@@ -351,7 +351,7 @@ ditango_status cross_sizes(ditango_dtype dt, int B, int H, int Hk, int D, int64_
   if (!valid_dtype(dt)) return DITANGO_ERR_INVALID;
   if (B < 1 || H < 1 || Hk < 1 || q_len < 1 || kv_len < 0 || H % Hk != 0) return DITANGO_ERR_INVALID;
   if (D != 64 && D != 128) return DITANGO_ERR_UNSUPPORTED;
-  if (q_len > (0x7fffffffLL - 1024) / H || kv_len > 0x7fffffffLL - 1024) return DITANGO_ERR_UNSUPPORTED;
+  if (H > 32768 || q_len > (0x7fffffffLL - 1024) / H || kv_len > 0x7fffffffLL - 1024) return DITANGO_ERR_UNSUPPORTED;
   memset(a, 0, sizeof(*a));
   a->q_len = q_len;
   a->B = B;
@@ -360,6 +360,7 @@ ditango_status cross_sizes(ditango_dtype dt, int B, int H, int Hk, int D, int64_
   a->G = H / Hk;
   a->kv_len = (int)kv_len;
   a->rows = (int)q_len * a->G;
+  a->g_inverse = a->G > 1 ? 0xffffffffu / (uint32_t)a->G + 1 : 0;
   return DITANGO_OK;
 }
 
@@ -399,8 +400,11 @@ ditango_status ditango_cross_attn(
   a.lens = kv_lens;
   a.mask = kv_len > 0 ? key_mask : nullptr;
   a.scale_log2 = scale * 1.4426950408889634f;
-  if (a.mask != nullptr && (!workspace || workspace_bytes < cross_list_bytes(a))) return DITANGO_ERR_INVALID;
-  return from_hip(launch_cross(a, dt, D, workspace, workspace != nullptr ? workspace_bytes : 0, (hipStream_t)stream));
+  if (!workspace) workspace_bytes = 0;
+  CrossPlan p;
+  if (plan_cross(a, dt, D, &p) != hipSuccess) return DITANGO_ERR_HIP;
+  if (workspace_bytes < p.need) return DITANGO_ERR_INVALID;
+  return from_hip(launch_cross(a, p, dt, D, workspace, workspace_bytes, (hipStream_t)stream));
 }
 
 size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk, int D, int64_t q_len,
@@ -409,8 +413,17 @@ size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk
   if (cross_sizes(dt, B, H, Hk, D, q_len, kv_len, &a) != DITANGO_OK) return 0;
   static const uint8_t dummy[1] = {0};
   a.mask = masked != 0 && kv_len > 0 ? dummy : nullptr;
-  CrossPlan p;
-  return plan_cross(a, dt, D, &p) == hipSuccess ? p.bytes : 0;
+  // which kernel a call runs depends on its strides too: room for either
+  a.q_head = D, a.q_token = (int64_t)H * D;
+  a.k_token = a.v_token = (int64_t)Hk * D;
+  size_t bytes = 0;
+  for (int i = 0; i < 2; ++i) {
+    CrossPlan p;
+    if (plan_cross(a, dt, D, &p) != hipSuccess) return 0;
+    bytes = p.bytes > bytes ? p.bytes : bytes;
+    a.q_token = INT64_MAX;       // no 32-bit offsets: the other kernel
+  }
+  return bytes;
 }
 
 ditango_status ditango_rotary(

@@ -1,6 +1,10 @@
 """Writes attn_d128_loop.inc and attn_d64_loop.inc: the key loop of the bf16
 attention kernel at head dim 128 and 64 as one block of gfx950 assembly
-each, scheduled by hand.
+each, scheduled by hand; and cross_d128_loop.inc and cross_d64_loop.inc, the
+same loop for workgroups that run one task after another (the cross
+attention's): Q^T comes in registers, the first tiles are in the ring, and the
+next task's Q^T is loaded into other registers while the last two key tiles
+are worked on.
 
 The loop computes, for one task (256 query rows of one head against the keys
 of one partition), the unnormalised attention state of Sec. 2.2.4
@@ -109,9 +113,15 @@ def Q(qb, s):                  # AGPR Q^T fragments
     return 128 + 32 * qb + 4 * s
 
 
+def QN(qb, s):                 # the next task's (task form)
+    return Q(qb, s) + 64
+
+
 # scalar registers: inputs pinned by the caller, then scratch
 S_SL2, S_NT, S_KVLEN, S_WLDS, S_TILEB, S_QSTAGE = 40, 41, 42, 44, 45, 46
 S_KD, S_VD = 48, 52            # buffer descriptors (4 each)
+S_QNEXT = 68                   # address of the next task's query rows (2; task form)
+V_QNEXT = 254                  # the lane's byte offsets from it, a query block each (2; task form)
 S_I, S_TMP, S_BIG, S_MASKAT, S_RET, S_CMP, S_NTM1, S_LIM = 56, 57, 58, 59, 60, 62, 64, 65
 SCRATCH_SGPRS = list(range(56, 66))
 
@@ -326,8 +336,9 @@ def desc_advance(desc):
 
 # ---------------------------------------------------------------- generator
 class Gen:
-    def __init__(self, fast=False):
+    def __init__(self, fast=False, task=False):
         self.fast = fast          # the fast form: no per-tile test of the running maximum
+        self.task = task          # the task form: Q^T in registers, the next task's loaded
         self.lines = []
         self.cold = []            # out-of-line code, emitted after the loop
         self.nlabel = 0
@@ -410,6 +421,11 @@ def iteration(g, u, tests=True):
     # the wave's own loads of the previous tile pair have landed (only this
     # iteration's 2 LW loads may be in flight)
     events.setdefault(BARRIER_STEP, []).extend([f"s_waitcnt vmcnt({2 * LW})", "s_barrier"])
+    if g.task and tests:
+        # iteration n-2: no tile follows
+        events.setdefault(BARRIER_STEP + 1, []).extend(
+            [f"s_add_u32 {s_(S_TMP)}, {s_(S_I)}, 1", f"s_cmp_eq_u32 {s_(S_TMP)}, {s_(S_NTM1)}"] +
+            g.out_of_line("s_cbranch_scc1", next_queries()))
     # the iteration's scalar bookkeeping, spread over its last steps (after
     # every load), then the exit test
     n = NQ + NP
@@ -428,9 +444,12 @@ def last_iteration(g, u):
     tile are drained first."""
     cur = u % 2
     g.lines += [f"{g.label(f'Llast{u}')}:", "s_waitcnt lgkmcnt(0)"]
+    newer = 2 * LW                # loads behind those of V_{n-1}
+    if g.task:
+        newer += 2 * KS           # the next task's queries
     g.lines += sm_ops(cur, 1, 0, False) + sm_ops(cur, 1, 1, False)
     g.lines += check_event(g, cur)
-    g.lines += [f"s_waitcnt vmcnt({2 * LW})", "s_barrier"]
+    g.lines += [f"s_waitcnt vmcnt({newer})", "s_barrier"]
     g.lines += stream(pv_steps(cur, u, 0), [], {}, {}, 0)
     g.lines += [f"s_branch {g.label('Ldone')}"]
 
@@ -518,12 +537,28 @@ def tile0_max():
     return out + ["s_nop 2"]
 
 
+def first_tiles():
+    out = []
+    for desc, ring, t in ((S_KD, KRING, 0), (S_KD, KRING, 1), (S_VD, VRING, 0), (S_KD, KRING, 2), (S_VD, VRING, 1)):
+        out += sum(dma_tile(desc, ring, t), []) + desc_advance(desc)
+    return out
+
+
+def next_queries():
+    """the next task's query rows, as Q^T fragments, into registers of their
+    own: issued when every tile of this task is on its way (behind the last
+    barrier but one), waited for where the block ends"""
+    return [f"global_load_dwordx4 {a_(QN(qb, s), 4)}, {v(V_QNEXT + qb)}, {s_(S_QNEXT, 2)}" + (f" offset:{32 * s}" if s else "")
+            for s in range(KS) for qb in range(2)]
+
+
 def prologue(g):
     L_ = g.lines
     L_ += ["s_nop 4"]
     # K_0, K_1, V_0, K_2, V_1 on their way, then everything that needs none
-    for desc, ring, t in ((S_KD, KRING, 0), (S_KD, KRING, 1), (S_VD, VRING, 0), (S_KD, KRING, 2), (S_VD, VRING, 1)):
-        L_ += sum(dma_tile(desc, ring, t), []) + desc_advance(desc)
+    # (task form: the workgroup has loaded them before)
+    if not g.task:
+        L_ += first_tiles()
     for qb in range(2):
         L_ += [f"v_mov_b32 {v(M(qb))}, 0xff800000", f"v_mov_b32 {v(L(qb))}, 0"]
     L_ += [f"v_accvgpr_write_b32 {a_(r)}, 0" for r in range(32 * DB)]
@@ -538,17 +573,18 @@ def prologue(g):
     # before the block) and K_0 have landed: only the later tiles may be in
     # flight.  Q^T fragments come from the staging space, laid out and
     # swizzled like a K tile's rows.
-    L_ += [f"s_waitcnt vmcnt({4 * LW})"]
-    for s in range(KS):
-        L_.append(f"v_add_u32 {v(QADDR + s)}, {s_(S_QSTAGE)}, {v(KADDR(s))}")
-    for qb in range(2):
+    if not g.task:
+        L_ += [f"s_waitcnt vmcnt({4 * LW})"]
         for s in range(KS):
-            L_.append(f"ds_read_b128 {v(32 * qb + 4 * s, 4)}, {v(QADDR + s)} offset:{qb * 32 * ROWB}")
-    L_ += ["s_waitcnt lgkmcnt(0)"]
-    for qb in range(2):
-        for s in range(KS):
-            for j in range(4):
-                L_.append(f"v_accvgpr_write_b32 {a_(Q(qb, s) + j)}, {v(32 * qb + 4 * s + j)}")
+            L_.append(f"v_add_u32 {v(QADDR + s)}, {s_(S_QSTAGE)}, {v(KADDR(s))}")
+        for qb in range(2):
+            for s in range(KS):
+                L_.append(f"ds_read_b128 {v(32 * qb + 4 * s, 4)}, {v(QADDR + s)} offset:{qb * 32 * ROWB}")
+        L_ += ["s_waitcnt lgkmcnt(0)"]
+        for qb in range(2):
+            for s in range(KS):
+                for j in range(4):
+                    L_.append(f"v_accvgpr_write_b32 {a_(Q(qb, s) + j)}, {v(32 * qb + 4 * s + j)}")
     # every wave's part of K_0 has landed, and every wave has read its Q rows
     # (the staging space is ring space that iteration 0 loads into)
     L_ += ["s_nop 2", "s_barrier"]
@@ -568,21 +604,24 @@ def prologue(g):
     if g.fast:
         L_ += tile0_max()
     L_ += sm_ops(0, 0, 0, True) + sm_ops(0, 0, 1, True)
+    if g.task:
+        L_ += [f"s_cmp_eq_u32 {s_(S_NT)}, 1"] + g.out_of_line("s_cbranch_scc1", next_queries())
     L_ += [f"s_cmp_eq_u32 {s_(S_NT)}, 1", f"s_cbranch_scc1 {g.label('Llast0')}"]
     # the last iteration a block of four may run: n-2, or n-3 when the last
     # tile is partial (iteration n-2 masks it); the first block runs if
     # iterations 0..3 fit below it
+    # (task form: n-3 in any case, iteration n-2 has its own event)
     L_ += [f"s_sub_i32 {s_(S_LIM)}, {s_(S_NT)}, 2",
            f"s_and_b32 {s_(S_TMP)}, {s_(S_KVLEN)}, 63",
-           f"s_cmp_lg_u32 {s_(S_TMP)}, 0",
-           f"s_cselect_b32 {s_(S_TMP)}, 1, 0",
+           *([f"s_mov_b32 {s_(S_TMP)}, 1"] if g.task else
+             [f"s_cmp_lg_u32 {s_(S_TMP)}, 0", f"s_cselect_b32 {s_(S_TMP)}, 1, 0"]),
            f"s_sub_i32 {s_(S_LIM)}, {s_(S_LIM)}, {s_(S_TMP)}",
            f"s_cmp_ge_i32 {s_(S_LIM)}, 3",
            f"s_cbranch_scc0 {g.label('Ltail')}"]
 
 
-def generate(fast=False):
-    g = Gen(fast)
+def generate(fast=False, task=False):
+    g = Gen(fast, task)
     prologue(g)
     # blocks of four steady iterations i..i+3 while i + 3 <= S_LIM
     g.lines += [f"{g.label('Lloop')}:"]
@@ -713,37 +752,44 @@ def check_fragments(lines):
     return problems
 
 
-def write(d):
+def write(d, name, task):
+    """The checked and the fast form of head dim d into {name}_d{d}_loop.inc."""
     configure(d)
-    forms = {"LOOP": generate(), "FAST": generate(fast=True)}
-    for name, lines in forms.items():
+    macro = f"DITANGO_{'CROSS_' if task else ''}D{d}"
+    forms = {"LOOP": generate(task=task), "FAST": generate(fast=True, task=task)}
+    for form, lines in forms.items():
         probs = check_hazards(lines) + check_fragments(lines)
         if probs:
             print("\n".join(probs[:40]))
-            print(f"D={d} {name}: {len(probs)} problems")
+            print(f"{name} D={d} {form}: {len(probs)} problems")
             sys.exit(1)
     here = os.path.dirname(os.path.abspath(__file__))
-    with open(os.path.join(here, f"attn_d{d}_loop.inc"), "w") as f:
+    with open(os.path.join(here, f"{name}_d{d}_loop.inc"), "w") as f:
         f.write("// Generated by gen_attn_loop.py from the schedule described there.\n")
-        for name, lines in forms.items():
-            f.write(f"// D={d} {name}: {len(lines)} lines, {sum(1 for x in lines if x.startswith('v_mfma'))} MFMAs.\n")
-            f.write(f"#define DITANGO_D{d}_{name}_ASM \\\n  \"")
+        for form, lines in forms.items():
+            f.write(f"// D={d} {form}: {len(lines)} lines, {sum(1 for x in lines if x.startswith('v_mfma'))} MFMAs.\n")
+            f.write(f"#define {macro}_{form}_ASM \\\n  \"")
             f.write("\\n\\t".join(lines))
             f.write("\\n\"\n")
+        if task:
+            lines = "\\n\\t".join(first_tiles())
+            f.write(f"// The first tiles' loads.\n#define {macro}_LOAD_ASM \\\n  \"{lines}\\n\"\n")
         # registers the block writes besides its outputs: scores,
-        # probabilities, fragments, temporaries, tile sums, the Q^T AGPRs,
-        # scalar scratch
+        # probabilities, fragments, temporaries, tile sums, the Q^T AGPRs
+        # (operands of the task form), scalar scratch
         clob = [f'"v{i}"' for i in range(0, 230)]
-        clob += [f'"a{i}"' for i in range(128, Q(1, KS - 1) + 4)]
+        if not task:
+            clob += [f'"a{i}"' for i in range(128, Q(1, KS - 1) + 4)]
         clob += [f'"s{i}"' for i in SCRATCH_SGPRS]
         clob += ['"m0"', '"vcc"', '"scc"', '"memory"']
-        f.write(f"#define DITANGO_D{d}_LOOP_CLOBBERS \\\n  " + ", ".join(clob) + "\n")
-    print(f"D={d}: {len(forms['LOOP'])} + {len(forms['FAST'])} lines")
+        f.write(f"#define {macro}_LOOP_CLOBBERS \\\n  " + ", ".join(clob) + "\n")
+    print(f"{name} D={d}: {len(forms['LOOP'])} + {len(forms['FAST'])} lines")
 
 
 def main():
     for d in (128, 64):
-        write(d)
+        write(d, "attn", False)
+        write(d, "cross", True)
 
 
 if __name__ == "__main__":

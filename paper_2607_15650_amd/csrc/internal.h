@@ -216,15 +216,20 @@ struct CrossArgs {
   int kv_len;               // keys of a sequence, at most
   int rows;                 // q_len * G
   int row_tiles;            // ceil(rows / rows per workgroup)
-  int split;                // key ranges, each a workgroup's
+  int split;                // key ranges, each a workgroup's: equal shares of
+  int chunk;                // a sequence's keys, or (> 0) this many each
+  uint32_t g_inverse;       // 2^32 / G, rounded up (G > 1)
   float scale_log2;
   const int32_t* lens;      // [B] live keys of a sequence (a prefix), or null
   const uint8_t* mask;      // [B][kv_len] or null
-  // the masked form, in the workspace: the live keys' places in order
-  // [B][kv_len], how many they are [B], and a row of zeros
-  int32_t* list;
+  // the masked form, in the workspace: how many keys are live [B], and either
+  // their places in order [B][kv_len] and a row of zeros, or their rows
+  // [B][kv_len][Hk][D]
   int32_t* count;
+  int32_t* list;
   float* zeros;
+  void* packed_k;
+  void* packed_v;
   // partial states of a split launch, in the workspace
   float* part_out;          // [split][B][H][q_len][D]
   float* part_lse;          // [split][B][H][q_len]
@@ -239,16 +244,24 @@ __device__ __forceinline__ int cross_keys(const CrossArgs& a, int b) {
 // How a launch of the cross attention runs on the current device, and the
 // workspace it takes.
 inline size_t align_up256(size_t x) { return (x + 255) & ~(size_t)255; }
-// of a masked call: the list, the counts and the zeros
-inline size_t cross_list_bytes(const CrossArgs& a) {
-  return a.mask == nullptr ? 0 : align_up256((size_t)a.B * a.kv_len * 4) + align_up256((size_t)a.B * 4) + 512;
-}
 struct CrossPlan {
-  int split;
+  // kRows: 128 rows a workgroup, key ranges in others; kTask: 256 rows, one
+  // after another (cross_task.hip; a masked call's live keys are packed for
+  // it); kResident: the head's keys in LDS (cross_resident.hip); kFew: chunks
+  // of keys (cross_few.hip)
+  enum Form { kRows, kTask, kResident, kFew } form;
+  int split, chunk;
+  size_t need;              // bytes of a masked call
   size_t bytes;             // with the partial states: without room for them the launch is not split
 };
 hipError_t plan_cross(const CrossArgs& a, ditango_dtype dt, int D, CrossPlan* p);
-hipError_t launch_cross(const CrossArgs& a, ditango_dtype dt, int D, void* ws, size_t ws_bytes, hipStream_t s);
+hipError_t launch_cross(const CrossArgs& a, const CrossPlan& p, ditango_dtype dt, int D, void* ws, size_t ws_bytes,
+                        hipStream_t s);
+bool cross_task_fits(const CrossArgs& a, int D);
+hipError_t launch_cross_task(const CrossArgs& a, int D, hipStream_t s);
+int cross_resident_keys(int D);     // at most
+hipError_t launch_cross_resident(const CrossArgs& a, int D, hipStream_t s);
+hipError_t launch_cross_few(const CrossArgs& a, int D, hipStream_t s);
 hipError_t launch_cross_f32(const CrossArgs& a, int D, hipStream_t s);
 int cross_f32_rows(int D);  // rows per workgroup
 

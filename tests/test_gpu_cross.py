@@ -21,27 +21,27 @@ pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
 
 
-def exact(q, k, v, scale, live):
-    """q [B, L, H, D], k, v [B, S, Hk, D], live bool [B, S] -> OUT, LSE in 64 bits on the CPU."""
-    q, k, v = (x.double().cpu() for x in (q, k, v))
+def exact(q, k, v, scale, live, device="cpu"):
+    """q [B, L, H, D], k, v [B, S, Hk, D], live bool [B, S] -> OUT, LSE in 64 bits."""
+    q, k, v = (x.double().to(device) for x in (q, k, v))
     B, L, H, D = q.shape
     G = H // k.shape[2]
-    out = torch.zeros(B, L, H, D, dtype=torch.float64)
-    lse = torch.full((B, H, L), -math.inf, dtype=torch.float64)
+    out = torch.zeros(B, L, H, D, dtype=torch.float64, device=device)
+    lse = torch.full((B, H, L), -math.inf, dtype=torch.float64, device=device)
     for b in range(B):
-        at = live[b].cpu().nonzero().flatten()
+        at = live[b].to(device).nonzero().flatten()
         if at.numel() == 0:
             continue
         for h in range(H):
-            s = q[b, :, h] @ k[b, at, h // G].T * scale
+            s = q[b, :, h] @ k[b, at, h // G].T.contiguous() * scale
             lse[b, h] = torch.logsumexp(s, 1)
             out[b, :, h] = torch.softmax(s, 1) @ v[b, at, h // G]
-    return out, lse
+    return out.cpu(), lse.cpu()
 
 
-def check(got, q, k, v, scale, live):
+def check(got, q, k, v, scale, live, device="cpu"):
     out, lse = (x.double().cpu() for x in got)
-    eo, el = exact(q, k, v, scale, live)
+    eo, el = exact(q, k, v, scale, live, device)
     lv = v.double().cpu()[live.cpu()]
     vm = float(lv.abs().max()) if lv.numel() else 0.0
     tol = (2.0 ** -7 + 2.0 ** -17) * vm if q.dtype == BF16 else 1e-5 * vm
@@ -132,6 +132,54 @@ def test_masks(gpu_lib, dtype, D, Lq, S, kind):
     both = mask & (torch.arange(S, device="cuda") < lens[:, None])
     kp, vp = poison(k, v, both)
     check(op(q, kp, vp, kv_lens=lens, key_mask=given), q, kp, vp, D ** -0.5, both)
+
+
+# many rows: few keys (kept in LDS), more (streamed), many (tasks one after another, whole or in key ranges)
+@pytest.mark.parametrize("kind", ["all", "lens", "mask"])
+@pytest.mark.parametrize("B,Lq,S,H,Hk,D", [
+    (2, 4500, 77, 24, 24, 128), (3, 2600, 320, 30, 10, 128), (1, 6000, 200, 36, 36, 64), (2, 3000, 640, 40, 20, 64),
+    (2, 2100, 333, 12, 12, 128), (2, 900, 513, 24, 24, 128), (3, 1000, 1100, 24, 8, 64), (3, 700, 2050, 20, 20, 128),
+    (2, 300, 6000, 6, 2, 128), (2, 500, 5000, 8, 8, 64),
+])
+def test_many_rows(gpu_lib, B, Lq, S, H, Hk, D, kind):
+    from paper_2607_15650_amd.cross import CrossAttention
+    q, k, v = make(B, Lq, S, H, Hk, D, BF16, seed=Lq, packed=kind == "lens")
+    live = torch.ones(B, S, dtype=torch.bool, device="cuda")
+    kw = {}
+    if kind == "lens":
+        lens = torch.tensor([S // 2 + 1, 0, S][:B], dtype=torch.int32, device="cuda")
+        live, kw = torch.arange(S, device="cuda") < lens[:, None], {"kv_lens": lens}
+    elif kind == "mask":
+        live = torch.rand(B, S, device="cuda") < 0.6
+        live[0] = False
+        live[0, S // 3] = True
+        kw = {"key_mask": live}
+    k, v = poison(k, v, live)
+    check(CrossAttention(D ** -0.5)(q, k, v, **kw), q, k, v, D ** -0.5, live, "cuda")
+
+
+@pytest.mark.parametrize("B,Lq,S,H,D", [(1, 9000, 100, 24, 128), (1, 13000, 300, 16, 64), (1, 2500, 900, 12, 128),
+                                        (1, 700, 3000, 8, 128), (1, 700, 3000, 8, 64), (1, 200, 400, 4, 128)])
+def test_many_rows_of_rising_scores(gpu_lib, B, Lq, S, H, D):
+    """The maximum of the first keys does not hold for the later ones, in some rows: they are raised or run again."""
+    from paper_2607_15650_amd.cross import CrossAttention
+    q, k, v = make(B, Lq, S, H, H, D, BF16, seed=11)
+    q[:, ::3] = q[:, ::3].abs()
+    ramp = (torch.arange(S, device="cuda").float() * (64 / S))[None, :, None, None].expand(B, S, H, D)
+    k = ramp.to(BF16).contiguous()
+    live = torch.ones(B, S, dtype=torch.bool, device="cuda")
+    out, lse = CrossAttention(0.125)(q, k, v)
+    eo, el = exact(q, k, v, 0.125, live, "cuda")
+    # scores up to 64 * sum|q| / 8 < 64 * 128 / 8 = 1024: off by 2^-24 * 1024 * 8 (growth of the sums) < 5e-4
+    assert float((lse.double().cpu() - el).abs().max()) <= 5e-4
+    assert float((out.double().cpu() - eo).abs().max()) <= (2 ** -7 + 1e-3) * float(v.abs().max())
+    # and a row whose scores are not numbers stays alone
+    q[0, 5, 1, 3] = float("nan")
+    again = CrossAttention(0.125)(q, k, v)
+    same = torch.ones(Lq, dtype=torch.bool, device="cuda")
+    same[5] = False
+    assert torch.isnan(again[0][0, 5, 1]).all() and torch.isnan(again[1][0, 1, 5])
+    assert float((again[0][:, same].double().cpu() - eo[:, same.cpu()]).abs().max()) <= (2 ** -7 + 1e-3) * float(v.abs().max())
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
