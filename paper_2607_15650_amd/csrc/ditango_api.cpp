@@ -401,6 +401,8 @@ ditango_status ditango_cross_attn(
   a.mask = kv_len > 0 ? key_mask : nullptr;
   a.scale_log2 = scale * 1.4426950408889634f;
   if (!workspace) workspace_bytes = 0;
+  // (what every kernel needs of a masked call: the live keys' number)
+  if (a.mask != nullptr && workspace_bytes < align_up256((size_t)B * 4) + 512) return DITANGO_ERR_INVALID;
   CrossPlan p;
   if (plan_cross(a, dt, D, &p) != hipSuccess) return DITANGO_ERR_HIP;
   if (workspace_bytes < p.need) return DITANGO_ERR_INVALID;
