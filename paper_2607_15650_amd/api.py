@@ -13,6 +13,7 @@ Layouts (all tensors contiguous, on the same GPU):
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -47,22 +48,33 @@ def _dev(*ts: torch.Tensor) -> None:
         raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
 
 
-def _dev_strided(*ts: torch.Tensor) -> None:
-    """_dev for tensors whose rows lie apart (only the last dim is dense)."""
-    dev = None
-    for t in ts:
+def _dev_strided(strided: Sequence[torch.Tensor], dense: Sequence[Optional[torch.Tensor]]) -> None:
+    """_dev for tensors whose rows lie apart (only their last dim is dense),
+    together with dense ones."""
+    dev = strided[0].device
+    # the kernels are enqueued on the current device's current stream
+    if dev.type != "cuda":
+        raise ValueError("all tensors must be on the GPU")
+    if dev.index != torch._C._cuda_getDevice():
+        raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
+    for t in strided:
+        if t.device != dev:
+            raise ValueError("all tensors must be on one device")
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError("the elements of a row must be contiguous")
+    for t in dense:
         if t is None:
             continue
-        if not t.is_cuda:
-            raise ValueError("all tensors must be on the GPU")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
+        if t.device != dev:
             raise ValueError("all tensors must be on one device")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
-            raise ValueError("the elements of a row must be contiguous")
-    if dev is not None and dev.index != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
+        if not t.is_contiguous():
+            raise ValueError("all tensors must be contiguous")
+
+
+# strides of [B, tokens, heads] as the C ABI takes them
+@functools.lru_cache(maxsize=256)
+def _strides(s0: int, s1: int, s2: int, s3: int):
+    return (ctypes.c_int64 * 3)(s0, s1, s2)
 
 
 def _stream() -> int:
@@ -307,10 +319,6 @@ def state_norms(out_states: torch.Tensor, norms: torch.Tensor, workspace: torch.
     _lib.check("ditango_state_norms", st)
 
 
-_I3 = ctypes.c_int64 * 3
-_DIMS = (64, 128)
-
-
 def cross_attn_workspace_bytes(dtype: torch.dtype, B: int, H: int, Hk: int, D: int, q_len: int, kv_len: int,
                                masked: bool = False) -> int:
     """Workspace bytes of cross_attn at these sizes on the current device."""
@@ -330,15 +338,12 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, 
     needs a ``workspace`` (uint8, 256-byte aligned) of
     cross_attn_workspace_bytes(...) bytes, another one splits the keys of a short
     query block with it."""
-    _dev_strided(q, k, v)
-    _dev(out, lse, kv_lens, key_mask, workspace)
-    if out.device != q.device:
-        raise ValueError("all tensors must be on one device")
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k and v must be [B, tokens, heads, D]")
+    _dev_strided((q, k, v), (out, lse, kv_lens, key_mask, workspace))
     B, q_len, H, D = q.shape
-    _, kv_len, Hk, _ = k.shape
-    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+    Bk, kv_len, Hk, Dk = k.shape
+    if k.shape != v.shape or Bk != B or Dk != D:
         raise ValueError("k/v shape mismatch")
     if Hk < 1 or H % Hk:
         raise ValueError("the query heads must be a multiple of the key/value heads")
@@ -359,7 +364,7 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, 
             raise ValueError(f"workspace too small: need {need} bytes")
     ws, n = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
     st = _lib.lib().ditango_cross_attn(
-        q.data_ptr(), _I3(*q.stride()[:3]), k.data_ptr(), _I3(*k.stride()[:3]), v.data_ptr(), _I3(*v.stride()[:3]),
+        q.data_ptr(), _strides(*q.stride()), k.data_ptr(), _strides(*k.stride()), v.data_ptr(), _strides(*v.stride()),
         _dtype(q), B, H, Hk, D, q_len, kv_len,
         kv_lens.data_ptr() if kv_lens is not None else None, key_mask.data_ptr() if key_mask is not None else None,
         float(scale), out.data_ptr(), lse.data_ptr() if lse is not None else None, ws, n, _stream())
@@ -381,35 +386,36 @@ def rotary(xs: Sequence[torch.Tensor], ys: Sequence[torch.Tensor], positions: to
     ``ys`` may be ``xs``.  ``positions`` int32 [1 or B, S, axes]; ``tables`` from
     rotary_tables; ``layout`` and ``norm`` as _lib names them; ``weights`` [D]
     (of each head) or [heads * D] (of the token's row)."""
-    if not 1 <= len(xs) <= 2 or len(ys) != len(xs):
+    n = len(xs)
+    if not 1 <= n <= 2 or len(ys) != n:
         raise ValueError("one or two tensors, and an output for each")
-    _dev_strided(*xs, *ys)
-    _dev(positions, *weights[:len(xs)])
-    B, S, _, D = xs[0].shape
-    if positions.device != xs[0].device:
-        raise ValueError("all tensors must be on one device")
+    x0 = xs[0]
+    if x0.dim() != 4:
+        raise ValueError("tensors must be [B, S, heads, D] of the same tokens, outputs like them")
+    _dev_strided((*xs, *ys), (positions, *weights[:n]))
+    B, S, _, D = x0.shape
+    dt = x0.dtype
     if positions.dtype != torch.int32 or positions.dim() != 3 or positions.shape[1] != S or \
             positions.shape[0] not in (1, B):
         raise ValueError("positions must be int32 [1 or B, S, axes]")
     if len(tables[0]) * 2 != rot_dim:
         raise ValueError("the tables must have one entry per pair of rot_dim")
-    arr = (_lib.RotaryTensor * len(xs))()
-    for i, (x, y) in enumerate(zip(xs, ys)):
+    arr = (_lib.RotaryTensor * n)()
+    for a, x, y, w in zip(arr, xs, ys, weights):
         if x.dim() != 4 or x.shape[0] != B or x.shape[1] != S or x.shape[3] != D or y.shape != x.shape:
             raise ValueError("tensors must be [B, S, heads, D] of the same tokens, outputs like them")
-        if x.dtype != xs[0].dtype or y.dtype != x.dtype:
+        if x.dtype != dt or y.dtype != dt:
             raise ValueError("the tensors must share a dtype")
-        w = weights[i] if norm != _lib.NORM_NONE else None
-        if norm != _lib.NORM_NONE:
-            need = D if norm == _lib.NORM_HEAD else x.shape[2] * D
-            if w is None or w.numel() != need or w.dtype != x.dtype:
-                raise ValueError(f"the norm needs {need} weights in the input dtype")
-        a = arr[i]
-        a.x, a.y, a.weight = x.data_ptr(), y.data_ptr(), w.data_ptr() if w is not None else None
-        a.x_strides[:], a.y_strides[:] = x.stride()[:3], y.stride()[:3]
         a.heads = x.shape[2]
+        if norm != _lib.NORM_NONE:
+            need = D if norm == _lib.NORM_HEAD else a.heads * D
+            if w is None or w.numel() != need or w.dtype != dt:
+                raise ValueError(f"the norm needs {need} weights in the input dtype")
+            a.weight = w.data_ptr()
+        a.x, a.y = x.data_ptr(), y.data_ptr()
+        a.x_strides, a.y_strides = _strides(*x.stride()), _strides(*y.stride())
     st = _lib.lib().ditango_rotary(
-        arr, len(xs), _dtype(xs[0]), B, S, D, positions.data_ptr(), positions.shape[0], positions.shape[2],
+        arr, n, _dtype(x0), B, S, D, positions.data_ptr(), positions.shape[0], positions.shape[2],
         tables[0], tables[1], rot_dim, layout, factor, norm, eps, _stream())
     _lib.check("ditango_rotary", st)
 

@@ -24,17 +24,17 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
 class CrossAttention:
     """Attention of query blocks to encoder states, with the workspace kept
     across calls (it only grows).  The calls of one instance share it: order
-    them on one stream, or across streams by events; a captured graph keeps the
-    workspace that was there when it was captured, so make the largest call
-    before the capture and no larger one until the graph is gone."""
+    them on one stream, or across streams by events.  A workspace that became
+    too small stays allocated, for graphs captured with it."""
 
     def __init__(self, scale: float):
         self.scale = float(scale)
         self._ws: Optional[torch.Tensor] = None
+        self._kept = []
         self._bytes = {}
 
     def _workspace(self, q, k, masked: bool) -> Optional[torch.Tensor]:
-        key = (q.dtype, q.shape, k.shape, masked, q.device)
+        key = (q.dtype, q.shape, k.shape, masked)
         n = self._bytes.get(key)
         if n is None:
             n = self._bytes[key] = api.cross_attn_workspace_bytes(
@@ -42,6 +42,8 @@ class CrossAttention:
         if n == 0:
             return None
         if self._ws is None or self._ws.numel() < n or self._ws.device != q.device:
+            if self._ws is not None:
+                self._kept.append(self._ws)
             self._ws = torch.empty(n, dtype=torch.uint8, device=q.device)
         return self._ws
 
@@ -51,7 +53,8 @@ class CrossAttention:
         live keys of k, v [B, kv_len, Hk, D].  Tensors that the kernels cannot
         read in place are copied first."""
         q, k, v = _rows(q), _rows(k), _rows(v)
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        B, q_len, H, D = q.shape
+        out = q.new_empty((B, q_len, H, D))
+        lse = q.new_empty((B, H, q_len), dtype=torch.float32)
         api.cross_attn(q, k, v, self.scale, out, lse, kv_lens, key_mask, self._workspace(q, k, key_mask is not None))
         return out, lse

@@ -279,6 +279,7 @@ struct RotaryArgs {
   float eps;
   // the launch: a team of threads per token
   int team;
+  int tokens;               // of a workgroup
   int units[2];             // of a token of each tensor
   double turns[DITANGO_ROTARY_MAX_PAIRS];    // of a pair, per position
   uint8_t axis[DITANGO_ROTARY_MAX_PAIRS];

@@ -11,9 +11,9 @@
 //   A team of threads per token, of both tensors (queries and keys of the same
 //   tokens share the angles).  The cosines and sines of a token, at most 64
 //   pairs, are formed once, by as many threads, and shared through LDS; the
-//   loads of the token's first elements are on their way meanwhile.  A thread
-//   takes units of two vectors: the two halves of VEC pairs.  A head's units
-//   lie in consecutive lanes, 4 ... 64 of them, which add up its squares
+//   loads of the token's first elements and weights are on their way meanwhile.
+//   A thread takes units of two vectors: the two halves of VEC pairs.  A head's
+//   units lie in consecutive lanes, 4 ... 64 of them, which add up its squares
 //   without LDS.
 //
 // Angles
@@ -33,11 +33,13 @@ template <typename T, int N> struct Vec {
 };
 template <typename T> struct Vec<T, 1> { typedef T type; };
 
-// VEC elements (a power of two) as floats
+// VEC elements (a power of two), as loaded, and as floats
 template <typename T, int VEC>
-__device__ __forceinline__ void load_vec(const T* p, float (&x)[VEC]) {
-  typedef typename Vec<T, VEC>::type V;
-  const V v = *(const V*)p;
+__device__ __forceinline__ typename Vec<T, VEC>::type load_raw(const T* p) {
+  return *(const typename Vec<T, VEC>::type*)p;
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void widen(const typename Vec<T, VEC>::type& v, float (&x)[VEC]) {
   if constexpr (VEC == 1) {
     x[0] = (float)v;
   } else {
@@ -58,7 +60,8 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[VEC]) {
   }
 }
 
-constexpr int kHeld = 2;      // units of a token that a thread holds
+// Units of a token that a thread holds: one of each tensor, or two of one.
+constexpr int kHeld = 2;
 
 template <typename T, int D, int VEC, bool HALF, int NORM>
 __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
@@ -69,36 +72,36 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
 
   const int tid = threadIdx.x;
   const int team = a.team;                    // threads of a token: below 64 a power of two, or all
-  const int in_team = tid % team, my = tid / team;
-  const int per_block = blockDim.x / team;
+  const int per_block = a.tokens;             // of a workgroup
+  const int in_team = per_block == 1 ? tid : tid & (team - 1), my = per_block == 1 ? 0 : tid / team;
   const int64_t tokens = (int64_t)a.B * a.S;
   const int64_t tok0 = (int64_t)blockIdx.x * per_block;
   const int64_t tok = tok0 + my;
   const bool live = tok < tokens;
-  const int64_t b = (live ? tok : 0) / a.S, s = (live ? tok : 0) % a.S;
+  // (a team without a token reads the last one's)
+  const int64_t at_tok = live ? tok : tokens - 1;
+  const int b = a.B == 1 ? 0 : (int)(at_tok / a.S);
+  const int64_t s = at_tok - b * a.S;
   const int pairs = a.rot >> 1;
-  const int all = a.units[0] + a.units[1];
 
-  // unit u of the token: its tensor, head and place in the head
+  // unit v of tensor k: its vectors, and those of its weights
   struct Place {
-    const T* x;
-    T* y;
-    const T* w;
-    int which, at, p0, p1;                    // unit in the head; its vectors' first elements
+    const T *x0, *x1, *w0, *w1;
+    T *y0, *y1;
+    int at;                                   // unit of the head
   };
-  auto place = [&](int u) {
-    Place p;
-    p.which = u >= a.units[0] ? 1 : 0;
-    const ditango_rotary_tensor& t = a.t[p.which];
-    const int v = u - (p.which ? a.units[0] : 0);
+  auto place = [&](int k, int v) {            // (k is the same for all threads)
+    const ditango_rotary_tensor& t = a.t[k];
     const int h = v / UD;
+    Place p;
     p.at = v % UD;
     const bool turn = p.at * VEC < pairs;
-    p.p0 = HALF && turn ? p.at * VEC : p.at * 2 * VEC;
-    p.p1 = HALF && turn ? p.p0 + pairs : p.p0 + VEC;
-    p.x = (const T*)t.x + b * t.x_strides[0] + s * t.x_strides[1] + h * t.x_strides[2];
-    p.y = (T*)t.y + b * t.y_strides[0] + s * t.y_strides[1] + h * t.y_strides[2];
-    p.w = (const T*)t.weight + (NORM == 2 ? h * D : 0);
+    const int p0 = HALF && turn ? p.at * VEC : p.at * 2 * VEC;
+    const int p1 = HALF && turn ? p0 + pairs : p0 + VEC;
+    const T* x = (const T*)t.x + b * t.x_strides[0] + s * t.x_strides[1] + h * t.x_strides[2];
+    T* y = (T*)t.y + b * t.y_strides[0] + s * t.y_strides[1] + h * t.y_strides[2];
+    const T* w = (const T*)t.weight + (NORM == 2 ? h * D : 0);
+    p.x0 = x + p0, p.x1 = x + p1, p.y0 = y + p0, p.y1 = y + p1, p.w0 = w + p0, p.w1 = w + p1;
     return p;
   };
   auto squares = [&](const float (&x0)[VEC], const float (&x1)[VEC]) {
@@ -107,25 +110,34 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
     for (int e = 0; e < VEC; ++e) q = __builtin_fmaf(x0[e], x0[e], __builtin_fmaf(x1[e], x1[e], q));
     return q;
   };
+  // tensor and unit of held slot i; the first unit of tensor k that is not held
+  const bool two = a.n == 2;
+  auto tensor_of = [&](int i) { return two ? i : 0; };
+  auto unit_of = [&](int i) { return two ? in_team : in_team + i * team; };
+  const int rest = two ? team : kHeld * team;
 
   // ---- the token's first units are on their way while the angles are formed
-  float x0[kHeld][VEC], x1[kHeld][VEC];
+  // (without a condition: a load under one is waited for inside it; a thread
+  // without a unit reads the tensor's last one)
+  typedef typename Vec<T, VEC>::type V;
+  V x0[kHeld], x1[kHeld], w0[kHeld], w1[kHeld];
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    const int u = in_team + i * team;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) x0[i][e] = x1[i][e] = 0.f;
-    if (live && u < all) {
-      const Place p = place(u);
-      load_vec<T, VEC>(p.x + p.p0, x0[i]);
-      load_vec<T, VEC>(p.x + p.p1, x1[i]);
+    const int k = tensor_of(i);
+    const Place p = place(k, min(unit_of(i), a.units[k] - 1));
+    x0[i] = load_raw<T, VEC>(p.x0);
+    x1[i] = load_raw<T, VEC>(p.x1);
+    if constexpr (NORM != 0) {
+      w0[i] = load_raw<T, VEC>(p.w0);
+      w1[i] = load_raw<T, VEC>(p.w1);
     }
   }
   for (int i = tid; i < per_block * pairs; i += blockDim.x) {
     const int64_t tk = tok0 + i / pairs;
     if (tk >= tokens) break;
     const int pr = i % pairs;
-    const double at = a.turns[pr] * (double)a.pos[(tk / a.S) * a.pos_batch + tk % a.S * a.axes + a.axis[pr]];
+    const int bk = a.B == 1 ? 0 : (int)(tk / a.S);
+    const double at = a.turns[pr] * (double)a.pos[bk * a.pos_batch + (tk - bk * a.S) * a.axes + a.axis[pr]];
     float sn, cs;
     sincospif(2.f * (float)(at - __builtin_rint(at)), &sn, &cs);
     turned[i] = float2{cs * a.factor, sn * a.factor};
@@ -137,18 +149,21 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
     float sq[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-      const float q = squares(x0[i], x1[i]);
-      if (in_team + i * team < a.units[0]) sq[0] += q; else sq[1] += q;
-    }
-    for (int u = in_team + kHeld * team; u < all; u += team) {
-      if (!live) break;
-      const Place p = place(u);
       float y0[VEC], y1[VEC];
-      load_vec<T, VEC>(p.x + p.p0, y0);
-      load_vec<T, VEC>(p.x + p.p1, y1);
-      const float q = squares(y0, y1);
-      if (p.which == 0) sq[0] += q; else sq[1] += q;
+      widen<T, VEC>(x0[i], y0);
+      widen<T, VEC>(x1[i], y1);
+      const float q = unit_of(i) < a.units[tensor_of(i)] ? squares(y0, y1) : 0.f;
+      if (tensor_of(i) == 0) sq[0] += q; else sq[1] += q;
     }
+    for (int k = 0; k < a.n; ++k)
+      for (int u = in_team + rest; u < a.units[k]; u += team) {
+        const Place p = place(k, u);
+        float y0[VEC], y1[VEC];
+        widen<T, VEC>(load_raw<T, VEC>(p.x0), y0);
+        widen<T, VEC>(load_raw<T, VEC>(p.x1), y1);
+        const float q = squares(y0, y1);
+        if (k == 0) sq[0] += q; else sq[1] += q;
+      }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       for (int d = 1; d < (team < 64 ? team : 64); d <<= 1) sq[k] += __shfl_xor(sq[k], d, 64);
@@ -167,21 +182,24 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
     __syncthreads();
   }
 
-  auto finish = [&](const Place& p, float (&y0)[VEC], float (&y1)[VEC]) {
+  auto finish = [&](const Place& p, float r, const V& x0, const V& x1, const V& w0, const V& w1) {
+    float y0[VEC], y1[VEC];
+    widen<T, VEC>(x0, y0);
+    widen<T, VEC>(x1, y1);
     if constexpr (NORM != 0) {
-      float w0[VEC], w1[VEC], r = p.which ? scale[1] : scale[0];
+      float v0[VEC], v1[VEC];
+      widen<T, VEC>(w0, v0);
+      widen<T, VEC>(w1, v1);
       if constexpr (NORM == 1) {
         float q = squares(y0, y1);
 #pragma unroll
         for (int d = 1; d < UD; d <<= 1) q += __shfl_xor(q, d, 64);
         r = rsqrtf(q * (1.f / D) + a.eps);
       }
-      load_vec<T, VEC>(p.w + p.p0, w0);
-      load_vec<T, VEC>(p.w + p.p1, w1);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        y0[e] = y0[e] * r * w0[e];
-        y1[e] = y1[e] * r * w1[e];
+        y0[e] = y0[e] * r * v0[e];
+        y1[e] = y1[e] * r * v1[e];
       }
     }
     if (p.at * VEC < pairs) {
@@ -196,44 +214,46 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
         u = t;
       }
     }
-    store_vec<T, VEC>(p.y + p.p0, y0);
-    store_vec<T, VEC>(p.y + p.p1, y1);
+    store_vec<T, VEC>(p.y0, y0);
+    store_vec<T, VEC>(p.y1, y1);
   };
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    const int u = in_team + i * team;
+    const int k = tensor_of(i), u = unit_of(i);
     // (a head's units are in or out together, so its lanes meet in the norm)
-    if (live && u < all) finish(place(u), x0[i], x1[i]);
+    if (live && u < a.units[k]) finish(place(k, u), k == 0 ? scale[0] : scale[1], x0[i], x1[i], w0[i], w1[i]);
   }
-  for (int u = in_team + kHeld * team; u < all; u += team) {
-    if (!live) break;
-    const Place p = place(u);
-    float y0[VEC], y1[VEC];
-    load_vec<T, VEC>(p.x + p.p0, y0);
-    load_vec<T, VEC>(p.x + p.p1, y1);
-    finish(p, y0, y1);
-  }
+  for (int k = 0; k < a.n; ++k)
+    for (int u = in_team + rest; u < a.units[k]; u += team) {
+      if (!live) break;
+      const Place p = place(k, u);
+      V v0 = {}, v1 = {};
+      if constexpr (NORM != 0) {
+        v0 = load_raw<T, VEC>(p.w0);
+        v1 = load_raw<T, VEC>(p.w1);
+      }
+      finish(p, k == 0 ? scale[0] : scale[1], load_raw<T, VEC>(p.x0), load_raw<T, VEC>(p.x1), v0, v1);
+    }
 }
 
 template <typename T, int D, int VEC, bool HALF, int NORM>
 hipError_t launch_vec(const RotaryArgs& a0, hipStream_t s) {
   RotaryArgs a = a0;
   constexpr int UD = D / (2 * VEC);
-  int all = 0;
-  for (int i = 0; i < a.n; ++i) all += a.units[i] = a.t[i].heads * UD;
-  // a team holds kHeld units a thread; teams below a wave are powers of two
-  // (their sums stay inside them), those above one are the workgroup
+  for (int i = 0; i < a.n; ++i) a.units[i] = a.t[i].heads * UD;
+  // a team holds a token's units where it can; teams of a wave or less are
+  // powers of two (their sums stay inside them), larger ones the workgroup
+  const int want = a.n == 2 ? (a.units[0] > a.units[1] ? a.units[0] : a.units[1]) : (a.units[0] + 1) / 2;
   int threads = 256;
-  const int want = (all + kHeld - 1) / kHeld;
-  if (want <= 32) {
+  if (want <= 64) {
     a.team = UD;
     while (a.team < want) a.team *= 2;
   } else {
     a.team = threads = want >= 1024 ? 1024 : (want + 63) / 64 * 64;
   }
-  const int64_t per_block = threads / a.team;
-  const int64_t grid = ((int64_t)a.B * a.S + per_block - 1) / per_block;
-  const size_t lds = (size_t)per_block * (a.rot / 2) * sizeof(float2);
+  a.tokens = threads / a.team;
+  const int64_t grid = ((int64_t)a.B * a.S + a.tokens - 1) / a.tokens;
+  const size_t lds = (size_t)a.tokens * (a.rot / 2) * sizeof(float2);
   hipLaunchKernelGGL((rotary_kernel<T, D, VEC, HALF, NORM>), dim3((unsigned)grid), dim3(threads), lds, s, a);
   return hipGetLastError();
 }

@@ -107,11 +107,11 @@ class Rotary:
         if positions.dim() != 3 or positions.shape[2] != len(self.axes):
             raise ValueError("positions must be int32 [1 or B, S, axes]")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = q.new_empty(q.shape)
         xs, ys = (q,), (q_out,)
         if k is not None:
             if k_out is None:
-                k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+                k_out = k.new_empty(k.shape)
             xs, ys = (q, k), (q_out, k_out)
         api.rotary(xs, ys, positions, self._tables, self.rot_dim, _LAYOUT[self.layout], self.factor, _NORM[self.norm],
                    (q_weight, k_weight), self.eps)
