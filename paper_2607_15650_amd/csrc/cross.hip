@@ -418,7 +418,7 @@ hipError_t plan_cross(const CrossArgs& a, ditango_dtype dt, int D, CrossPlan* p)
   } else {
     // a launch that leaves half the compute units idle splits its keys, two
     // tiles at least in each range
-    const int bm = cross_f32_rows(D);
+    const int bm = cross_f32_rows(a, D, cus);
     const int64_t groups = (int64_t)((a.rows + bm - 1) / bm) * a.Hk * a.B, tiles = (a.kv_len + 63) / 64;
     const int64_t split = 2 * groups <= cus ? 2 * (int64_t)cus / groups : 1;
     p->split = (int)(split < tiles / 2 ? split : tiles / 2 > 1 ? tiles / 2 : 1);

@@ -3,9 +3,9 @@
 // MFMAs) over rows that are strided or listed, and the same second pass with
 // the float32 MFMA where the planes cannot hold a value.
 //
-// A workgroup is four waves and 32 rows of one key/value head: the waves
-// split the keys of its range, stage their own tiles without barriers, and
-// compose their partial states through LDS.
+// As there, a workgroup has RW x KW waves: RW of them share the key tiles, 32
+// rows each, or (RW = 1) KW of them split the keys of its range, stage their own
+// tiles without barriers, and compose their partial states through LDS.
 #include "attn_f32_loop.h"
 #include "internal.h"
 
@@ -15,7 +15,6 @@ namespace {
 template <class C, class Rows>
 __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArgs a) {
   constexpr int D = C::D;
-  static_assert(C::RW == 1 && C::KW > 1, "the waves split the keys");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
 
   int t = xcd_remap(blockIdx.x, gridDim.x);
@@ -43,14 +42,16 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
   vr.stride = a.v_token;
   if constexpr (Rows::kListed) kr.list = vr.list = a.list + (int64_t)b * a.kv_len;
 
-  const int row = rt * C::BM + lr;
+  const int row = rt * C::BM + (C::KW == 1 ? wave * 32 : 0) + lr;
   const bool row_ok = row < a.rows;
   const int tok = min(row, a.rows - 1) / a.G, gi = min(row, a.rows - 1) % a.G;
   const float* qrow = (const float*)a.q + b * a.q_batch + tok * a.q_token + (int64_t)(hk * a.G + gi) * a.q_head;
 
+  const int kw = C::KW == 1 ? 0 : wave;
   const int per = (te - tb + C::KW - 1) / C::KW;
-  const int t0 = min(tb + wave * per, te), t1 = min(t0 + per, te);
-  unsigned char* kb = smem + wave * C::GROUP;
+  const int t0 = min(tb + kw * per, te), t1 = min(t0 + per, te);
+  unsigned char* kb = smem + kw * C::GROUP;
+  const int gt = C::KW == 1 ? tid : lane;
   float* part_m = (float*)(smem + C::KW * C::GROUP);
   float* part_l = part_m + C::KW * 32;
   int* redo = (int*)(part_l + C::KW * 32);
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
   float m, l;
   if (tid < 3) redo[tid] = 0;
   uint64_t ask = 0;
-  key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, lane, o, m, l, ask);
+  key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
   // what the planes cannot hold, as attn_f32_kernel finds it
   float bad = l * 0.f, low = INFINITY;
 #pragma unroll
@@ -98,12 +99,37 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
     again = __builtin_amdgcn_readfirstlane(redo[2]) != 0;
   }
   if (again) {
-    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, lane, o, m, l, ask);
+    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
     __syncthreads();
   }
 
-  // partial states through LDS: O rows of 16-byte units, swizzled by row
   const float lt = pair_sum(l);
+  if constexpr (C::KW == 1) {
+    if (row_ok) {
+      const float inv = lt > 0.f ? 1.0f / lt : 0.f;
+      const float lse = lt > 0.f ? (m + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
+      const int h = hk * a.G + gi;
+      const int64_t at = ((int64_t)b * a.H + h) * a.q_len + tok, ap = (int64_t)sp * a.B * a.H * a.q_len + at;
+      float* dst = (a.split > 1 ? a.part_out + ap * D : (float*)a.out + (((int64_t)b * a.q_len + tok) * a.H + h) * D) + 4 * g;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = o[db][4 * r4 + e] * inv;
+          *(f32x4*)(dst + db * 32 + 8 * r4) = x;
+        }
+      if (g == 0) {
+        if (a.split > 1)
+          a.part_lse[ap] = lse;
+        else if (a.lse != nullptr)
+          a.lse[at] = lse;
+      }
+    }
+    return;
+  } else {
+  // partial states through LDS: O rows of 16-byte units, swizzled by row
   float* po = (float*)kb;
 #pragma unroll
   for (int db = 0; db < C::DB; ++db)
@@ -153,6 +179,7 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
       if (u == 0 && a.lse != nullptr) a.lse[at] = lse;
     }
   }
+  }
 }
 
 template <class C, class Rows>
@@ -172,13 +199,37 @@ hipError_t launch_f32_rows(const CrossArgs& a0, hipStream_t s) {
 
 }  // namespace
 
-int cross_f32_rows(int) { return 32; }
+// The form of a launch, by how its workgroups fill the compute units, as the
+// float32 attention chooses it (attn_f32.hip): 32 rows and the waves on the
+// keys up to two rounds, then 128 rows while every workgroup has a compute unit
+// to itself, then 256 (D=64: 128).  2,047 rows x 12 heads against 333 keys at
+// D=128: 32 rows 61 us, 128 rows 45 us.
+using Split128 = CfgF<128, 1, 4, 1, false>;
+using Mid128 = CfgF<128, 4, 1, 1, true>;
+using Shared128 = CfgF<128, 8, 1, 2, false>;
+using Split64 = CfgF<64, 1, 8, 2, false>;
+using Shared64 = CfgF<64, 4, 1, 2, true>;
+
+int cross_f32_rows(const CrossArgs& a, int D, int cus) {
+  const int64_t heads = (int64_t)a.Hk * a.B;
+  if ((int64_t)(a.rows + 31) / 32 * heads <= 2 * (int64_t)cus) return 32;
+  if (D == 64 || (int64_t)(a.rows + 127) / 128 * heads <= cus) return 128;
+  return 256;
+}
 
 hipError_t launch_cross_f32(const CrossArgs& a, int D, hipStream_t s) {
-  using C128 = CfgF<128, 1, 4, 1, false>;
-  using C64 = CfgF<64, 1, 8, 2, false>;
-  if (D == 128) return a.mask ? launch_f32_rows<C128, ListedRows>(a, s) : launch_f32_rows<C128, StridedRows>(a, s);
-  return a.mask ? launch_f32_rows<C64, ListedRows>(a, s) : launch_f32_rows<C64, StridedRows>(a, s);
+  int dev = 0, cus = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e != hipSuccess) return e;
+  const int rows = cross_f32_rows(a, D, cus);
+  if (D == 64) {
+    if (rows == 32) return a.mask ? launch_f32_rows<Split64, ListedRows>(a, s) : launch_f32_rows<Split64, StridedRows>(a, s);
+    return a.mask ? launch_f32_rows<Shared64, ListedRows>(a, s) : launch_f32_rows<Shared64, StridedRows>(a, s);
+  }
+  if (rows == 32) return a.mask ? launch_f32_rows<Split128, ListedRows>(a, s) : launch_f32_rows<Split128, StridedRows>(a, s);
+  if (rows == 128) return a.mask ? launch_f32_rows<Mid128, ListedRows>(a, s) : launch_f32_rows<Mid128, StridedRows>(a, s);
+  return a.mask ? launch_f32_rows<Shared128, ListedRows>(a, s) : launch_f32_rows<Shared128, StridedRows>(a, s);
 }
 
 }  // namespace ditango

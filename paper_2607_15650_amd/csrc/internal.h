@@ -263,7 +263,7 @@ int cross_resident_keys(int D);     // at most
 hipError_t launch_cross_resident(const CrossArgs& a, int D, hipStream_t s);
 hipError_t launch_cross_few(const CrossArgs& a, int D, hipStream_t s);
 hipError_t launch_cross_f32(const CrossArgs& a, int D, hipStream_t s);
-int cross_f32_rows(int D);  // rows per workgroup
+int cross_f32_rows(const CrossArgs& a, int D, int cus);   // rows per workgroup
 
 // One launch of the rotary positions.
 struct RotaryArgs {

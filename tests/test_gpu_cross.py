@@ -158,6 +158,24 @@ def test_many_rows(gpu_lib, B, Lq, S, H, Hk, D, kind):
     check(CrossAttention(D ** -0.5)(q, k, v, **kw), q, k, v, D ** -0.5, live, "cuda")
 
 
+@pytest.mark.parametrize("kind", ["all", "lens", "mask"])
+@pytest.mark.parametrize("B,Lq,S,H,Hk,D", [(2, 1047, 333, 12, 12, 128), (2, 2500, 130, 24, 12, 128), (2, 1500, 97, 24, 24, 64)])
+def test_many_rows_f32(gpu_lib, B, Lq, S, H, Hk, D, kind):
+    from paper_2607_15650_amd.cross import CrossAttention
+    q, k, v = make(B, Lq, S, H, Hk, D, F32, seed=Lq, packed=True)
+    live = torch.ones(B, S, dtype=torch.bool, device="cuda")
+    kw = {}
+    if kind == "lens":
+        lens = torch.tensor([S - 32, 0], dtype=torch.int32, device="cuda")
+        live, kw = torch.arange(S, device="cuda") < lens[:, None], {"kv_lens": lens}
+    elif kind == "mask":
+        live = torch.rand(B, S, device="cuda") < 0.6
+        kw = {"key_mask": live}
+    k, v = poison(k, v, live)
+    q[0, 7] *= 1e-36                       # values that the planes do not hold
+    check(CrossAttention(D ** -0.5)(q, k, v, **kw), q, k, v, D ** -0.5, live, "cuda")
+
+
 @pytest.mark.parametrize("B,Lq,S,H,D", [(1, 9000, 100, 24, 128), (1, 13000, 300, 16, 64), (1, 2500, 900, 12, 128),
                                         (1, 700, 3000, 8, 128), (1, 700, 3000, 8, 64), (1, 200, 400, 4, 128)])
 def test_many_rows_of_rising_scores(gpu_lib, B, Lq, S, H, D):
