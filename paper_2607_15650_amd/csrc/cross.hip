@@ -456,7 +456,7 @@ hipError_t launch_cross(const CrossArgs& a0, const CrossPlan& p, ditango_dtype d
       a.k_batch = a.v_batch = a.kv_len * a.k_token;
       a.lens = a.count;
       a.mask = nullptr;
-    } else {
+    } else if (p.form != CrossPlan::kResident || !cross_resident_lists(a, D)) {
       a.list = (int32_t*)at;
       a.zeros = (float*)(at + align_up256(keys * 4));
       hipLaunchKernelGGL(cross_list_kernel, dim3(a.B), dim3(1024), 0, s, a);

@@ -6,7 +6,6 @@
 // walk over blocks of query rows by themselves, without a barrier: while one
 // wave of a SIMD takes exponentials the other's products run.  The next
 // block's queries are on their way from the last use of this one's on.
-#include <stdlib.h>
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -16,6 +15,8 @@
 namespace ditango {
 namespace {
 
+constexpr int kLds = 163840;                        // of a compute unit
+
 template <int D_, int NW_>
 struct ResidentCfg {
   static constexpr int D = D_, NW = NW_, BN = 64;
@@ -24,11 +25,16 @@ struct ResidentCfg {
   static constexpr int UNITS = D / 8, ROWB = D * 2, TILEB = BN * ROWB;
   static constexpr int RPL = 1024 / ROWB;
   static constexpr int LOADS = TILEB / 1024;       // 1 KiB loads of a tile
-  static constexpr int MAX_TILES = 163840 / (2 * TILEB);
-  static constexpr int LDS = MAX_TILES * 2 * TILEB;
+  static constexpr int MAX_TILES = kLds / (2 * TILEB);
 };
 
-template <class C, bool LIST>
+// How the keys' rows are found: a prefix; the list of the workspace; or the
+// mask, whose live keys the workgroup lists behind its tiles in LDS (the
+// launch of a kernel for that alone took 6 us of 81: 14,850 rows x 48 heads at
+// D=64, 256 of 333 keys live).
+enum Keys { kPrefix, kList, kMask };
+
+template <class C, Keys KEYS>
 __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const CrossArgs) {
   constexpr int D = C::D, BN = C::BN;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -55,12 +61,38 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
     const int first = (int)(at - (int64_t)grp * a->row_tiles);
     const int last = (int)min((int64_t)a->row_tiles, first + (end - at));   // row blocks [first, last)
     at += last - first;
-    const int n = __builtin_amdgcn_readfirstlane(live_keys(a, b));
+    __syncthreads();                                    // the head before is done with
+    int n;
+    int* own_list = (int*)(smem + (a->kv_len + BN - 1) / BN * 2 * C::TILEB);
+    if constexpr (KEYS == kMask) {
+      // places of the live keys, in order: counts by ballot, waves in order
+      int* sums = own_list + a->kv_len;
+      const int keys = a->lens == nullptr ? a->kv_len : min(max(a->lens[b], 0), a->kv_len);
+      const uint8_t* mask = a->mask + (int64_t)b * a->kv_len;
+      n = 0;
+      for (int k0 = 0; k0 < keys; k0 += C::NT) {
+        const int key = k0 + tid;
+        const bool live = key < keys && mask[key] != 0;
+        const uint64_t votes = __builtin_amdgcn_ballot_w64(live);
+        if (lane == 0) sums[wave] = __builtin_popcountll(votes);
+        __syncthreads();
+        int before = n;
+#pragma unroll
+        for (int v = 0; v < C::NW; ++v) {
+          if (v < wave) before += sums[v];
+          n += sums[v];
+        }
+        if (live) own_list[before + __builtin_popcountll(votes & ((1ull << lane) - 1))] = key;
+        __syncthreads();
+      }
+      n = __builtin_amdgcn_readfirstlane(n);
+    } else {
+      n = __builtin_amdgcn_readfirstlane(live_keys(a, b));
+    }
     const int tiles = (n + BN - 1) / BN, steps = (n + 31) / 32;
     const float sl2 = a->scale_log2;
 
     // ---- K and V of the head: tile i of K, then of V
-    __syncthreads();                                    // the head before is done with
     const __bf16* kg = (const __bf16*)a->k + b * a->k_batch + hk * a->k_head;
     const __bf16* vg = (const __bf16*)a->v + b * a->v_batch + hk * a->v_head;
     for (int u = wave; u < tiles * 2 * C::LOADS; u += C::NW) {
@@ -70,10 +102,15 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
       const uint32_t dst = lds0 + (uint32_t)((2 * i + which) * C::TILEB + j * 1024);
       const int r = j * C::RPL + ld_row;
       const int unit = ld_unit ^ (which ? swz_v<D>(r) : swz_k<D>(r));
-      if constexpr (LIST) {
+      if constexpr (KEYS == kList) {
         const __bf16* p = (const __bf16*)a->zeros;
         if (i * BN + r < n) p = base + a->list[(int64_t)b * a->kv_len + i * BN + r] * stride;
         dma_addr(p + unit * 8, dst);
+      } else if constexpr (KEYS == kMask) {
+        // (places past the last live key lie past the descriptor's end)
+        const u32x4 desc = buffer_desc(base, (uint32_t)((a->kv_len - 1) * stride * 2 + C::ROWB));
+        const uint32_t row = i * BN + r < n ? (uint32_t)own_list[i * BN + r] * (uint32_t)(stride * 2) : 0x80000000u;
+        dma_desc(desc, row + (uint32_t)unit * 16, dst);
       } else {
         const u32x4 desc = buffer_desc(base + (int64_t)i * BN * stride,
                                        (uint32_t)min((int64_t)(n - 1 - i * BN) * stride * 2 + C::ROWB, (int64_t)0x7fffffff));
@@ -135,17 +172,22 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
   }
 }
 
-template <class C, bool LIST>
+template <class C>
+size_t resident_lds(const CrossArgs& a, bool mask) {
+  return (size_t)(a.kv_len + C::BN - 1) / C::BN * 2 * C::TILEB + (mask ? (size_t)a.kv_len * 4 + C::NW * 4 : 0);
+}
+
+template <class C, Keys KEYS>
 hipError_t launch_resident(const CrossArgs& a0, int cus, int dev, hipStream_t s) {
-  const hipError_t e = set_kernel_lds<&cross_resident_kernel<C, LIST>, C::LDS>(dev);
+  const hipError_t e = set_kernel_lds<&cross_resident_kernel<C, KEYS>, kLds>(dev);
   if (e != hipSuccess) return e;
   CrossArgs a = a0;
   a.row_tiles = (a.rows + C::BM - 1) / C::BM;
   const int64_t all = (int64_t)a.row_tiles * a.Hk * a.B;
   const int64_t want = (all + C::NW - 1) / C::NW;
   const int grid = (int)(want < cus ? want : cus);
-  const size_t lds = (size_t)(a.kv_len + C::BN - 1) / C::BN * 2 * C::TILEB;
-  hipLaunchKernelGGL((cross_resident_kernel<C, LIST>), dim3((unsigned)grid), dim3(C::NT), lds, s, a);
+  hipLaunchKernelGGL((cross_resident_kernel<C, KEYS>), dim3((unsigned)grid), dim3(C::NT),
+                     resident_lds<C>(a, KEYS == kMask), s, a);
   return hipGetLastError();
 }
 
@@ -156,18 +198,24 @@ using Resident64 = ResidentCfg<64, 16>;
 
 int cross_resident_keys(int D) { return (D == 128 ? Resident128::MAX_TILES : Resident64::MAX_TILES) * 64; }
 
+bool cross_resident_lists(const CrossArgs& a, int D) {
+  const int64_t stride = a.k_token > a.v_token ? a.k_token : a.v_token;
+  const size_t lds = D == 128 ? resident_lds<Resident128>(a, true) : resident_lds<Resident64>(a, true);
+  return lds <= (size_t)kLds && a.kv_len * stride * 2 < ((int64_t)1 << 31);
+}
+
+template <class C>
+static hipError_t launch_form(const CrossArgs& a, int D, int cus, int dev, hipStream_t s) {
+  if (a.mask == nullptr) return launch_resident<C, kPrefix>(a, cus, dev, s);
+  return cross_resident_lists(a, D) ? launch_resident<C, kMask>(a, cus, dev, s) : launch_resident<C, kList>(a, cus, dev, s);
+}
+
 hipError_t launch_cross_resident(const CrossArgs& a, int D, hipStream_t s) {
   int dev = 0, cus = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e == hipSuccess) e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess) return e;
-#ifdef SWEEP
-  const int cfg = getenv("RES") ? atoi(getenv("RES")) : 0;
-  if (D == 128 && cfg == 1) return launch_resident<ResidentCfg<128, 8>, false>(a, cus, dev, s);
-  if (D == 64 && cfg == 1) return launch_resident<ResidentCfg<64, 12>, false>(a, cus, dev, s);
-#endif
-  if (D == 128) return a.mask ? launch_resident<Resident128, true>(a, cus, dev, s) : launch_resident<Resident128, false>(a, cus, dev, s);
-  return a.mask ? launch_resident<Resident64, true>(a, cus, dev, s) : launch_resident<Resident64, false>(a, cus, dev, s);
+  return D == 128 ? launch_form<Resident128>(a, D, cus, dev, s) : launch_form<Resident64>(a, D, cus, dev, s);
 }
 
 }  // namespace ditango

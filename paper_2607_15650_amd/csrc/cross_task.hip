@@ -355,7 +355,7 @@ asm volatile(BODY                                                               
       if (t.row0 + r < a->rows) {
         int tok, gi;
         token_of(a, t.row0, r, &tok, &gi);
-        *(bf16x8*)(out + ((int64_t)tok * a->H + gi) * D) = x[i];
+        __builtin_nontemporal_store(x[i], (bf16x8*)(out + ((int64_t)tok * a->H + gi) * D));
       }
     }
     if (next == task) break;

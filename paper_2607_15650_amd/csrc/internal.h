@@ -260,6 +260,7 @@ hipError_t launch_cross(const CrossArgs& a, const CrossPlan& p, ditango_dtype dt
 bool cross_task_fits(const CrossArgs& a, int D);
 hipError_t launch_cross_task(const CrossArgs& a, int D, hipStream_t s);
 int cross_resident_keys(int D);     // at most
+bool cross_resident_lists(const CrossArgs& a, int D);   // a masked call lists its live keys by itself
 hipError_t launch_cross_resident(const CrossArgs& a, int D, hipStream_t s);
 hipError_t launch_cross_few(const CrossArgs& a, int D, hipStream_t s);
 hipError_t launch_cross_f32(const CrossArgs& a, int D, hipStream_t s);

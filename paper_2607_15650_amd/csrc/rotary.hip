@@ -56,7 +56,7 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[VEC]) {
     V v;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) v[e] = (T)x[e];
-    *(V*)p = v;
+    __builtin_nontemporal_store(v, (V*)p);
   }
 }
 
