@@ -65,13 +65,17 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   int lane = lane_id();
   int lr = lane & 31, g = lane >> 5;
 
-  // this workgroup's tasks: every (gridDim / 8)-th of its XCD's contiguous
-  // eighth, so that the XCD's workgroups share the K and V rows of a head
-  const int n_tasks = a->row_tiles * a->Hk * a->B * a->split;
+  // This workgroup's tasks: of every class (the tasks of a sequence and key
+  // range, or all where these are few) its XCD takes a contiguous eighth, whose
+  // workgroups then share the K and V rows of a head, and the workgroup every
+  // (gridDim / 8)-th of the eighths in turn: sequences of different lengths are
+  // shared out evenly (2 x 4,095 rows x 12 heads against 512 and 77 keys 35 ->
+  // 31 us).
   const int xcd = blockIdx.x & 7, step = gridDim.x >> 3;
-  const int first = xcd_first(xcd, n_tasks), end = first + xcd_len(xcd, n_tasks);
-  int task = first + (blockIdx.x >> 3);
-  if (task >= end) return;
+  const int eighth = xcd_len(xcd, a->class_tasks), end = eighth * a->classes;
+  int at = blockIdx.x >> 3;                          // in the XCD's list
+  if (at >= end) return;
+  auto task_at = [&](Args a, int i) { return i / eighth * a->class_tasks + xcd_first(xcd, a->class_tasks) + i % eighth; };
 
   // a task's sequence, key/value head, first row and key range
   struct Rows {
@@ -81,10 +85,10 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
     Rows r;
     r.row0 = t % a->row_tiles * C::BM;
     t /= a->row_tiles;
-    r.b = t % a->B;
-    t /= a->B;
     r.hk = t % a->Hk;
-    r.part = t / a->Hk;
+    t /= a->Hk;
+    r.b = t % a->B;
+    r.part = t / a->B;
     return r;
   };
   // its keys, and the first of them
@@ -175,6 +179,7 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   if (threadIdx.x < 3) redo[threadIdx.x] = 0;
   int turn = 0;
 
+  int task = task_at(a, at), next_task;
   query_rows(a, rows_of(a, task));
   load_queries();
   int key0, n = keys_of(a, rows_of(a, task), &key0);
@@ -185,11 +190,12 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   for (;;) {
     a = args();
     Rows t = rows_of(a, task);
-    const int next = task + step < end ? task + step : task;
+    const bool more = at + step < end;
+    next_task = more ? task_at(a, at + step) : task;
     f32x16 q[C::NQ];
 #pragma unroll
     for (int i = 0; i < C::NQ; ++i) q[i] = qn[i];
-    query_rows(a, rows_of(a, next));
+    query_rows(a, rows_of(a, next_task));
     const int clear = turn == 2 ? 0 : turn + 1;
     if (wave == 0 && lane == 0) redo[clear] = 0;
 
@@ -261,7 +267,7 @@ asm volatile(BODY                                                               
       load_queries();
 #pragma unroll
       for (int i = 0; i < C::NQ; ++i) q[i] = qn[i];
-      query_rows(a, rows_of(a, next));
+      query_rows(a, rows_of(a, next_task));
       first_tiles(a, t, key0, n, &kd, &vd);
       landed();
       key_loop(std::true_type{});
@@ -273,8 +279,8 @@ asm volatile(BODY                                                               
     // the next task's first tiles come in while this one's rows go out; the
     // rows' stores wait for them, because the waits of the loop go by order
     const bool keys = n > 0;
-    n = keys_of(a, rows_of(a, next), &key0);
-    first_tiles(a, rows_of(a, next), key0, n, &kd, &vd);
+    n = keys_of(a, rows_of(a, next_task), &key0);
+    first_tiles(a, rows_of(a, next_task), key0, n, &kd, &vd);
     lane = lane_id();
     lr = lane & 31, g = lane >> 5;
 
@@ -304,8 +310,9 @@ asm volatile(BODY                                                               
             a->part_lse[at] = lt > 0.f ? (m[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
         }
       }
-      if (next == task) break;
-      task = next;
+      if (!more) break;
+      at += step;
+      task = next_task;
       continue;
     }
     // ---- the rows' state: through LDS (16-byte units swizzled by row, the
@@ -358,8 +365,9 @@ asm volatile(BODY                                                               
         __builtin_nontemporal_store(x[i], (bf16x8*)(out + ((int64_t)tok * a->H + gi) * D));
       }
     }
-    if (next == task) break;
-    task = next;
+    if (!more) break;
+    at += step;
+    task = next_task;
   }
 }
 
@@ -372,7 +380,11 @@ hipError_t launch_task(const CrossArgs& a0, int cus, int dev, hipStream_t s) {
   a.row_tiles = (a.rows + C::BM - 1) / C::BM;
   const int64_t tasks = (int64_t)a.row_tiles * a.Hk * a.B * a.split;
   if (tasks > 0x7fffffff - 4096) return hipErrorInvalidConfiguration;
-  const int64_t per_xcd = (tasks + 7) / 8, most = cus / 8 > 0 ? cus / 8 : 1;
+  // classes where each gives an XCD eight tasks
+  const int64_t one = (int64_t)a.row_tiles * a.Hk;
+  a.class_tasks = (int)(one >= 64 ? one : tasks);
+  a.classes = one >= 64 ? a.B * a.split : 1;
+  const int64_t per_xcd = (int64_t)a.classes * ((a.class_tasks + 7) / 8), most = cus / 8 > 0 ? cus / 8 : 1;
   const int grid = (int)(8 * (per_xcd < most ? per_xcd : most));
   hipLaunchKernelGGL((cross_task_kernel<D>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);
   return hipGetLastError();

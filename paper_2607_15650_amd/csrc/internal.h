@@ -219,6 +219,8 @@ struct CrossArgs {
   int split;                // key ranges, each a workgroup's: equal shares of
   int chunk;                // a sequence's keys, or (> 0) this many each
   uint32_t g_inverse;       // 2^32 / G, rounded up (G > 1)
+  int class_tasks;          // of the task kernel: the tasks of a class, and
+  int classes;              // the classes
   float scale_log2;
   const int32_t* lens;      // [B] live keys of a sequence (a prefix), or null
   const uint8_t* mask;      // [B][kv_len] or null
