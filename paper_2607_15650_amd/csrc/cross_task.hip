@@ -52,6 +52,14 @@ __device__ __forceinline__ int lane_id() {
   asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
   return x;
 }
+// x / d for wave-uniform 0 <= x < 2^31, with 2^32 / d rounded down (d = 1:
+// 2^32 - 1): the product's high half is the quotient or one less.
+__device__ __forceinline__ int divide(int x, int d, uint32_t inverse) {
+  const int q = (int)__umulhi((uint32_t)x, inverse);
+  return q + (x - q * d >= d ? 1 : 0);
+}
+inline uint32_t inverse_of(int d) { return d == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d); }
+
 template <int D_>
 __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   using C = TaskCfg<D_>;
@@ -75,7 +83,12 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   const int eighth = xcd_len(xcd, a->class_tasks), end = eighth * a->classes;
   int at = blockIdx.x >> 3;                          // in the XCD's list
   if (at >= end) return;
-  auto task_at = [&](Args a, int i) { return i / eighth * a->class_tasks + xcd_first(xcd, a->class_tasks) + i % eighth; };
+  const int eighth_first = xcd_first(xcd, a->class_tasks);
+  const uint32_t eighth_inverse = eighth == 1 ? 0xffffffffu : __builtin_amdgcn_readfirstlane(0xffffffffu / (uint32_t)eighth);
+  auto task_at = [&](Args a, int i) {
+    const int c = divide(i, eighth, eighth_inverse);
+    return c * a->class_tasks + eighth_first + (i - c * eighth);
+  };
 
   // a task's sequence, key/value head, first row and key range
   struct Rows {
@@ -83,12 +96,11 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   };
   auto rows_of = [](Args a, int t) {
     Rows r;
-    r.row0 = t % a->row_tiles * C::BM;
-    t /= a->row_tiles;
-    r.hk = t % a->Hk;
-    t /= a->Hk;
-    r.b = t % a->B;
-    r.part = t / a->B;
+    const int u = divide(t, a->row_tiles, a->tiles_inverse), w = divide(u, a->Hk, a->heads_inverse);
+    r.row0 = (t - u * a->row_tiles) * C::BM;
+    r.hk = u - w * a->Hk;
+    r.part = divide(w, a->B, a->batch_inverse);
+    r.b = w - r.part * a->B;
     return r;
   };
   // its keys, and the first of them
@@ -179,23 +191,22 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
   if (threadIdx.x < 3) redo[threadIdx.x] = 0;
   int turn = 0;
 
-  int task = task_at(a, at), next_task;
-  query_rows(a, rows_of(a, task));
+  Rows t = rows_of(a, task_at(a, at));
+  query_rows(a, t);
   load_queries();
-  int key0, n = keys_of(a, rows_of(a, task), &key0);
+  int key0, n = keys_of(a, t, &key0);
   u32x4 kd, vd;
-  first_tiles(a, rows_of(a, task), key0, n, &kd, &vd);
+  first_tiles(a, t, key0, n, &kd, &vd);
   landed();
   __syncthreads();
   for (;;) {
     a = args();
-    Rows t = rows_of(a, task);
     const bool more = at + step < end;
-    next_task = more ? task_at(a, at + step) : task;
+    const Rows next = more ? rows_of(a, task_at(a, at + step)) : t;
     f32x16 q[C::NQ];
 #pragma unroll
     for (int i = 0; i < C::NQ; ++i) q[i] = qn[i];
-    query_rows(a, rows_of(a, next_task));
+    query_rows(a, next);
     const int clear = turn == 2 ? 0 : turn + 1;
     if (wave == 0 && lane == 0) redo[clear] = 0;
 
@@ -267,7 +278,7 @@ asm volatile(BODY                                                               
       load_queries();
 #pragma unroll
       for (int i = 0; i < C::NQ; ++i) q[i] = qn[i];
-      query_rows(a, rows_of(a, next_task));
+      query_rows(a, next);
       first_tiles(a, t, key0, n, &kd, &vd);
       landed();
       key_loop(std::true_type{});
@@ -275,12 +286,11 @@ asm volatile(BODY                                                               
     }
     turn = clear;
     a = args();
-    t = rows_of(a, task);
     // the next task's first tiles come in while this one's rows go out; the
     // rows' stores wait for them, because the waits of the loop go by order
     const bool keys = n > 0;
-    n = keys_of(a, rows_of(a, next_task), &key0);
-    first_tiles(a, rows_of(a, next_task), key0, n, &kd, &vd);
+    n = keys_of(a, next, &key0);
+    first_tiles(a, next, key0, n, &kd, &vd);
     lane = lane_id();
     lr = lane & 31, g = lane >> 5;
 
@@ -312,7 +322,7 @@ asm volatile(BODY                                                               
       }
       if (!more) break;
       at += step;
-      task = next_task;
+      t = next;
       continue;
     }
     // ---- the rows' state: through LDS (16-byte units swizzled by row, the
@@ -355,19 +365,31 @@ asm volatile(BODY                                                               
             l[qb] > 0.f ? (m[qb] + __builtin_amdgcn_logf(l[qb])) * kLn2 : l[qb] == 0.f ? -INFINITY : l[qb];
       }
     }
+    const int64_t out_row_elems = (int64_t)a->H * D;
     __bf16* out = (__bf16*)a->out + ((int64_t)t.b * a->q_len * a->H + t.hk * a->G) * D + out_unit * 8;
+    if (a->G == 1) {
+      // rows at a fixed distance
+      const int r0 = t.row0 + wave * QB * 32 + out_row;
+      __bf16* p = out + r0 * out_row_elems;
 #pragma unroll
-    for (int i = 0; i < QB * 32 / C::RPL; ++i) {
-      const int r = wave * QB * 32 + i * C::RPL + out_row;
-      if (t.row0 + r < a->rows) {
-        int tok, gi;
-        token_of(a, t.row0, r, &tok, &gi);
-        __builtin_nontemporal_store(x[i], (bf16x8*)(out + ((int64_t)tok * a->H + gi) * D));
+      for (int i = 0; i < QB * 32 / C::RPL; ++i) {
+        if (r0 + i * C::RPL < a->rows) __builtin_nontemporal_store(x[i], (bf16x8*)p);
+        p += C::RPL * out_row_elems;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < QB * 32 / C::RPL; ++i) {
+        const int r = wave * QB * 32 + i * C::RPL + out_row;
+        if (t.row0 + r < a->rows) {
+          int tok, gi;
+          token_of(a, t.row0, r, &tok, &gi);
+          __builtin_nontemporal_store(x[i], (bf16x8*)(out + tok * out_row_elems + gi * D));
+        }
       }
     }
     if (!more) break;
     at += step;
-    task = next_task;
+    t = next;
   }
 }
 
@@ -384,6 +406,9 @@ hipError_t launch_task(const CrossArgs& a0, int cus, int dev, hipStream_t s) {
   const int64_t one = (int64_t)a.row_tiles * a.Hk;
   a.class_tasks = (int)(one >= 64 ? one : tasks);
   a.classes = one >= 64 ? a.B * a.split : 1;
+  a.tiles_inverse = inverse_of(a.row_tiles);
+  a.heads_inverse = inverse_of(a.Hk);
+  a.batch_inverse = inverse_of(a.B);
   const int64_t per_xcd = (int64_t)a.classes * ((a.class_tasks + 7) / 8), most = cus / 8 > 0 ? cus / 8 : 1;
   const int grid = (int)(8 * (per_xcd < most ? per_xcd : most));
   hipLaunchKernelGGL((cross_task_kernel<D>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);

@@ -420,11 +420,17 @@ def iteration(g, u, tests=True):
     pre = {NQ: check_event(g, cur) + (mask_event(g, nxt) if tests else [])}
     # the wave's own loads of the previous tile pair have landed (only this
     # iteration's 2 LW loads may be in flight)
-    events.setdefault(BARRIER_STEP, []).extend([f"s_waitcnt vmcnt({2 * LW})", "s_barrier"])
+    wait = [f"s_waitcnt vmcnt({2 * LW})"]
     if g.task and tests:
-        # iteration n-2: no tile follows
+        # iteration n-2: the next task's queries are in flight as well
+        more, back = g.uniq("Lcold"), g.uniq("Lback")
+        g.cold += [f"{more}:", f"s_waitcnt vmcnt({2 * LW + 2 * KS})", f"s_branch {back}"]
+        wait = [f"s_add_u32 {s_(S_TMP)}, {s_(S_I)}, 1", f"s_cmp_eq_u32 {s_(S_TMP)}, {s_(S_NTM1)}",
+                f"s_cbranch_scc1 {more}"] + wait + [f"{back}:"]
+    events.setdefault(BARRIER_STEP, []).extend(wait + ["s_barrier"])
+    if g.task and tests:
         events.setdefault(BARRIER_STEP + 1, []).extend(
-            [f"s_add_u32 {s_(S_TMP)}, {s_(S_I)}, 1", f"s_cmp_eq_u32 {s_(S_TMP)}, {s_(S_NTM1)}"] +
+            [f"s_add_u32 {s_(S_TMP)}, {s_(S_I)}, 2", f"s_cmp_eq_u32 {s_(S_TMP)}, {s_(S_NTM1)}"] +
             g.out_of_line("s_cbranch_scc1", next_queries()))
     # the iteration's scalar bookkeeping, spread over its last steps (after
     # every load), then the exit test
@@ -447,10 +453,18 @@ def last_iteration(g, u):
     newer = 2 * LW                # loads behind those of V_{n-1}
     if g.task:
         newer += 2 * KS           # the next task's queries
-    g.lines += sm_ops(cur, 1, 0, False) + sm_ops(cur, 1, 1, False)
-    g.lines += check_event(g, cur)
-    g.lines += [f"s_waitcnt vmcnt({newer})", "s_barrier"]
-    g.lines += stream(pv_steps(cur, u, 0), [], {}, {}, 0)
+    if g.task and g.fast:
+        # the exponentials beside the products of the first key block
+        valu = {}
+        valu.update(spread_valu(sm_ops(cur, 1, 0, False), 0, NP // 4))
+        valu.update(spread_valu(sm_ops(cur, 1, 1, False), NP // 4, NP // 4))
+        g.lines += [f"s_waitcnt vmcnt({newer})", "s_barrier"]
+        g.lines += stream(pv_steps(cur, u, 0), [], valu, {NP // 2: check_event(g, cur)}, 0)
+    else:
+        g.lines += sm_ops(cur, 1, 0, False) + sm_ops(cur, 1, 1, False)
+        g.lines += check_event(g, cur)
+        g.lines += [f"s_waitcnt vmcnt({newer})", "s_barrier"]
+        g.lines += stream(pv_steps(cur, u, 0), [], {}, {}, 0)
     g.lines += [f"s_branch {g.label('Ldone')}"]
 
 
@@ -517,7 +531,7 @@ def mask_block(g, par):
     c += ["s_nop 1", f"s_setpc_b64 {s_(S_RET, 2)}"]
 
 
-def tile0_max():
+def tile0_max(three=False):
     """m of each query block = scale*log2(e) times the row maximum of tile
     0's scores (both key blocks, the two lanes of a row combined), the value
     the slow path gives m at tile 0 in the checked form"""
@@ -525,8 +539,12 @@ def tile0_max():
     for qb in range(2):
         regs = [S(0, kb, qb) + r for kb in range(2) for r in range(16)]
         out.append(f"v_max_f32 {v(TMP)}, {v(regs[0])}, {v(regs[1])}")
-        for r in regs[2:]:
-            out.append(f"v_max_f32 {v(TMP)}, {v(TMP)}, {v(r)}")
+        if three:                 # two at a time
+            for r in range(2, 32, 2):
+                out.append(f"v_max3_f32 {v(TMP)}, {v(TMP)}, {v(regs[r])}, {v(regs[r + 1])}")
+        else:
+            for r in regs[2:]:
+                out.append(f"v_max_f32 {v(TMP)}, {v(TMP)}, {v(r)}")
         out += [f"v_mov_b32 {v(TMP + 1)}, {v(TMP)}",
                 "s_nop 1",
                 f"v_permlane32_swap_b32 {v(TMP)}, {v(TMP + 1)}",
@@ -546,8 +564,9 @@ def first_tiles():
 
 def next_queries():
     """the next task's query rows, as Q^T fragments, into registers of their
-    own: issued when every tile of this task is on its way (behind the last
-    barrier but one), waited for where the block ends"""
+    own: issued in iteration n-3, behind its barrier, when the last tile that
+    counts is on its way; the waits after it leave them in flight, and they are
+    waited for where the block ends"""
     return [f"global_load_dwordx4 {a_(QN(qb, s), 4)}, {v(V_QNEXT + qb)}, {s_(S_QNEXT, 2)}" + (f" offset:{32 * s}" if s else "")
             for s in range(KS) for qb in range(2)]
 
@@ -561,7 +580,9 @@ def prologue(g):
         L_ += first_tiles()
     for qb in range(2):
         L_ += [f"v_mov_b32 {v(M(qb))}, 0xff800000", f"v_mov_b32 {v(L(qb))}, 0"]
-    L_ += [f"v_accvgpr_write_b32 {a_(r)}, 0" for r in range(32 * DB)]
+    zero = [f"v_accvgpr_write_b32 {a_(r)}, 0" for r in range(32 * DB)]
+    if not g.task:
+        L_ += zero
     L_ += [f"s_mov_b32 {s_(S_BIG)}, 0x53800000", f"s_mov_b32 {s_(S_I)}, 0",
            f"s_sub_u32 {s_(S_NTM1)}, {s_(S_NT)}, 1",
            # the steady iteration that masks the next tile: n-2 if the last tile is partial
@@ -589,8 +610,10 @@ def prologue(g):
     # (the staging space is ring space that iteration 0 loads into)
     L_ += ["s_nop 2", "s_barrier"]
     # scores of tile 0 while K_1 and V_0 arrive
-    L_ += stream(qk_steps(0, 0), [], {}, {}, 0)
-    L_ += [f"s_waitcnt vmcnt({2 * LW})", "s_barrier"]
+    # (task form: all of them are here, and O is cleared meanwhile)
+    L_ += stream(qk_steps(0, 0), [], spread_valu(zero, 0, NQ) if g.task else {}, {}, 0)
+    if not g.task:
+        L_ += [f"s_waitcnt vmcnt({2 * LW})", "s_barrier"]
     # the reads of iteration 0's first steps
     for st in qk_steps(1, 1)[:LA]:
         L_ += st.reads
@@ -602,18 +625,18 @@ def prologue(g):
         f"s_cbranch_scc1 {g.label('Lpmaskskip')}"] + g.call_seq(g.label("Lmask0")) + [f"{g.label('Lpmaskskip')}:"])
     L_ += ["s_nop 7", "s_nop 7"]
     if g.fast:
-        L_ += tile0_max()
+        L_ += tile0_max(g.task)
     L_ += sm_ops(0, 0, 0, True) + sm_ops(0, 0, 1, True)
     if g.task:
-        L_ += [f"s_cmp_eq_u32 {s_(S_NT)}, 1"] + g.out_of_line("s_cbranch_scc1", next_queries())
+        L_ += [f"s_cmp_le_u32 {s_(S_NT)}, 2"] + g.out_of_line("s_cbranch_scc1", next_queries())
     L_ += [f"s_cmp_eq_u32 {s_(S_NT)}, 1", f"s_cbranch_scc1 {g.label('Llast0')}"]
     # the last iteration a block of four may run: n-2, or n-3 when the last
     # tile is partial (iteration n-2 masks it); the first block runs if
     # iterations 0..3 fit below it
-    # (task form: n-3 in any case, iteration n-2 has its own event)
+    # (task form: n-4, the iterations n-3 and n-2 have their own events)
     L_ += [f"s_sub_i32 {s_(S_LIM)}, {s_(S_NT)}, 2",
            f"s_and_b32 {s_(S_TMP)}, {s_(S_KVLEN)}, 63",
-           *([f"s_mov_b32 {s_(S_TMP)}, 1"] if g.task else
+           *([f"s_mov_b32 {s_(S_TMP)}, 2"] if g.task else
              [f"s_cmp_lg_u32 {s_(S_TMP)}, 0", f"s_cselect_b32 {s_(S_TMP)}, 1, 0"]),
            f"s_sub_i32 {s_(S_LIM)}, {s_(S_LIM)}, {s_(S_TMP)}",
            f"s_cmp_ge_i32 {s_(S_LIM)}, 3",

@@ -221,6 +221,7 @@ struct CrossArgs {
   uint32_t g_inverse;       // 2^32 / G, rounded up (G > 1)
   int class_tasks;          // of the task kernel: the tasks of a class, and
   int classes;              // the classes
+  uint32_t tiles_inverse, heads_inverse, batch_inverse;   // of its divisions
   float scale_log2;
   const int32_t* lens;      // [B] live keys of a sequence (a prefix), or null
   const uint8_t* mask;      // [B][kv_len] or null
