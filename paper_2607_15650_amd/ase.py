@@ -31,6 +31,7 @@ import numpy as np
 import torch
 
 from . import api
+from .rotary import RotatedInputs, Rotary, check_rotary_args
 from .workspace import AttnWorkspace
 from .groups import base_groups
 
@@ -64,7 +65,7 @@ def accuracy_stats(predicted: Sequence[float], measured: Sequence[float]) -> Dic
 class ErrorModelSelectiveAttention:
     def __init__(self, B: int, H: int, D: int, offsets: Sequence[int], q: int, g: int, scale: float,
                  reuse_ratio: float, eps_local: float, dtype=torch.bfloat16, device="cuda",
-                 evaluate: bool = False):
+                 evaluate: bool = False, rotary: Optional[Rotary] = None):
         self.B, self.H, self.D = B, H, D
         self.offsets = [int(o) for o in offsets]
         self.P = len(self.offsets) - 1
@@ -96,6 +97,7 @@ class ErrorModelSelectiveAttention:
         nws = max(api.norms_workspace_bytes(B, H, D, self.L, self.P), api.contrib_workspace_bytes(B, H, self.L, self.P))
         self._ws = torch.empty(max(16, nws), dtype=torch.uint8, device=device)
         self._attn_ws = AttnWorkspace(device)
+        self._rotated = RotatedInputs(rotary, self.offsets, q) if rotary is not None else None
 
     # ---------------------------------------------------------------- helpers
     def _norms(self, states: torch.Tensor, slots: Sequence[int], ref: Optional[torch.Tensor] = None) -> List[float]:
@@ -113,6 +115,8 @@ class ErrorModelSelectiveAttention:
     def _attn(self, qb, k, v, sel, states, lses):
         """qb: (query tensor, the block's first row in it)"""
         q, q0 = qb
+        if self._rotated is not None:
+            k = self._rotated.keys(sel)
         ws = self._attn_ws.get(q.dtype, q.shape[0], q.shape[2], q.shape[3], self.L, self.offsets, sel)
         api.attn_block_states(q, q0, self.L, k, v, self.offsets, sel, self.scale, states, lses, ws)
 
@@ -122,11 +126,17 @@ class ErrorModelSelectiveAttention:
             api.merge_states(states, lses, states[a], lses[a], slots=list(range(*grp)))
 
     # ---------------------------------------------------------------- one step
-    def step(self, t: int, q_all: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
+    def step(self, t: int, q_all: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+             positions: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+             k_weight: Optional[torch.Tensor] = None):
         """Returns (OUT, LSE, info) with info = dict(anchor, compute, ase, eps, drift), and,
         when the model is evaluated, ``measured`` (group -> the error its cached
         state actually carries) at every step after the first."""
-        qb = api.query_block(q_all, self.offsets[self.q], self.L)
+        check_rotary_args(self._rotated, positions, q_weight, k_weight)
+        if self._rotated is not None:
+            qb = self._rotated.begin(q_all, k, positions, q_weight, k_weight), 0
+        else:
+            qb = api.query_block(q_all, self.offsets[self.q], self.L)
         loc = [0] * self.P
         loc[self.q] = 1
         self._attn(qb, k, v, loc, self.cache, self.cache_lse)          # local partition first

@@ -23,6 +23,7 @@ from typing import List, Optional, Sequence, Tuple
 import torch
 
 from . import api
+from .rotary import RotatedInputs, Rotary, check_rotary_args
 from .workspace import AttnWorkspace
 
 
@@ -60,12 +61,12 @@ def compose_pairs(groups: Sequence[Tuple[int, int]], q: int, k: int = 2) -> List
 
 class GroupedSelectiveAttention:
     """Selective attention with group-granular state reuse for one query block.
-    The steps of one instance share its states and workspaces: order them on one
+    ``rotary`` as SelectiveAttention takes it.  The steps of one instance share its states and workspaces: order them on one
     stream, or across streams by events."""
 
     def __init__(self, B: int, H: int, D: int, offsets: Sequence[int], q: int, g: int, scale: float,
                  dtype: torch.dtype = torch.bfloat16, device="cuda",
-                 mem_budget_bytes: Optional[int] = None, k: int = 2):
+                 mem_budget_bytes: Optional[int] = None, k: int = 2, rotary: Optional[Rotary] = None):
         self.B, self.H, self.D = B, H, D
         self.offsets = [int(o) for o in offsets]
         self.P = len(self.offsets) - 1
@@ -80,6 +81,7 @@ class GroupedSelectiveAttention:
         self.groups = base_groups(self.P, q, g)
         self.computed_at = {grp: -1 for grp in self.groups}
         self._ws = None
+        self._rotated = RotatedInputs(rotary, self.offsets, q) if rotary is not None else None
 
     @property
     def state_bytes(self) -> int:
@@ -122,10 +124,12 @@ class GroupedSelectiveAttention:
         return n
 
     def step(self, step: int, q_all: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
-             compute: Sequence[Tuple[int, int]]):
+             compute: Sequence[Tuple[int, int]], positions: Optional[torch.Tensor] = None,
+             q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None):
         """One step: the groups in ``compute`` (and the local partition) get fresh
         states, the others are reused; returns (OUT, LSE, weights per live group
         in the order of ``self.groups`` followed by the local partition)."""
+        check_rotary_args(self._rotated, positions, q_weight, k_weight)
         compute = set(compute)
         sel = [0] * self.P
         sel[self.q] = 1
@@ -135,7 +139,11 @@ class GroupedSelectiveAttention:
                     sel[j] = 1
         a = self.offsets[self.q]
         ws = self._attn_ws.get(q_all.dtype, self.B, self.H, self.D, self.L, self.offsets, sel)
-        q, q0 = api.query_block(q_all, a, self.L)
+        if self._rotated is not None:
+            q, q0 = self._rotated.begin(q_all, k, positions, q_weight, k_weight), 0
+            k = self._rotated.keys(sel)
+        else:
+            q, q0 = api.query_block(q_all, a, self.L)
         api.attn_block_states(q, q0, self.L, k, v, self.offsets, sel, self.scale, self.out, self.lse, ws)
         for grp in self.groups:
             if grp in compute:

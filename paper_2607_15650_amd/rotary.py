@@ -116,3 +116,60 @@ class Rotary:
         api.rotary(xs, ys, positions, self._tables, self.rot_dim, _LAYOUT[self.layout], self.factor, _NORM[self.norm],
                    (q_weight, k_weight), self.eps)
         return (q_out, k_out) if k is not None else q_out
+
+
+class RotatedInputs:
+    """The rotated query block and keys of an engine's step, in buffers of its
+    own.  Only the rows that the step reads are rotated: the block, and the keys
+    of the partitions computed fresh (those of the block's own partition in the
+    same call as its queries)."""
+
+    def __init__(self, rotary: Rotary, offsets: Sequence[int], qb: int):
+        self.rotary = rotary
+        self.offsets = [int(o) for o in offsets]
+        self.qb = qb
+        self.q: Optional[torch.Tensor] = None
+        self.k: Optional[torch.Tensor] = None
+
+    def begin(self, q_all: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+              q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor]) -> torch.Tensor:
+        """Starts a step with its tensors ([B, S, H, D], positions [1 or B, S,
+        axes]): returns the rotated query block [B, L, H, D].  The block's own
+        keys are rotated with it."""
+        a, e = self.offsets[self.qb], self.offsets[self.qb + 1]
+        if positions is None or positions.dim() != 3 or positions.shape[1] != k.shape[1] or \
+                k.shape[1] != self.offsets[-1]:
+            raise ValueError("an engine with rotary positions needs positions [1 or B, S, axes] of the whole sequence")
+        B, H, D = q_all.shape[0], q_all.shape[2], q_all.shape[3]
+        if self.q is None or self.q.shape != (B, e - a, H, D) or self.q.dtype != q_all.dtype or self.q.device != q_all.device:
+            self.q = q_all.new_empty((B, e - a, H, D))
+        if self.k is None or self.k.shape != k.shape or self.k.dtype != k.dtype or self.k.device != k.device:
+            self.k = k.new_empty(k.shape)
+        self._src, self._pos, self._kw = k, positions, k_weight
+        self._done = {self.qb}
+        if e > a:
+            self.rotary(q_all[:, a:e], k[:, a:e], positions[:, a:e].contiguous(), q_weight, k_weight, self.q,
+                        self.k[:, a:e])
+        return self.q
+
+    def keys(self, select: Sequence[int]) -> torch.Tensor:
+        """K [B, S, H, D] with the rows of the selected partitions rotated."""
+        P = len(self.offsets) - 1
+        j = 0
+        while j < P:
+            if not select[j] or j in self._done:
+                j += 1
+                continue
+            i = j
+            while j < P and select[j] and j not in self._done:
+                self._done.add(j)
+                j += 1
+            a, e = self.offsets[i], self.offsets[j]
+            if e > a:
+                self.rotary(self._src[:, a:e], None, self._pos[:, a:e].contiguous(), self._kw, q_out=self.k[:, a:e])
+        return self.k
+
+
+def check_rotary_args(rotary: Optional[Rotary], positions, q_weight, k_weight) -> None:
+    if rotary is None and (positions is not None or q_weight is not None or k_weight is not None):
+        raise ValueError("positions and norm weights belong to an engine with rotary positions")

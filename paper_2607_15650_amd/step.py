@@ -10,11 +10,12 @@ and calls them in order on the current stream.
 """
 from __future__ import annotations
 
-from typing import List, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
 from . import api
+from .rotary import RotatedInputs, Rotary, check_rotary_args
 from .workspace import AttnWorkspace
 
 
@@ -35,13 +36,18 @@ class SelectiveAttention:
     cached states: the input dtype (default) or float32 for bf16 inputs; the
     composed output is in the input dtype either way.
 
+    With ``rotary`` the steps take queries and keys as the projections leave
+    them, and their positions (``rotary.Rotary``: the norm of queries and keys
+    and their rotation); a step then rotates the query block and the keys of the
+    partitions it computes fresh, into buffers kept for the query block.
+
     The steps of one instance share its workspaces, whatever the query block:
     order them on one stream, or across streams by events.
     """
 
     def __init__(self, B: int, H: int, D: int, offsets: Sequence[int], scale: float,
                  dtype: torch.dtype = torch.bfloat16, device="cuda",
-                 state_dtype: torch.dtype = None):
+                 state_dtype: torch.dtype = None, rotary: Optional[Rotary] = None):
         self.B, self.H, self.D = B, H, D
         self.offsets = [int(o) for o in offsets]
         self.P = len(self.offsets) - 1
@@ -50,6 +56,8 @@ class SelectiveAttention:
         self.state_dtype = state_dtype if state_dtype is not None else dtype
         self.device = device
         self.caches = {}
+        self.rotary = rotary
+        self._rotated = {}
         self._ws = {}
         self._attn_ws = AttnWorkspace(device)
 
@@ -60,16 +68,27 @@ class SelectiveAttention:
         return self.caches[qb]
 
     def step(self, step: int, qb: int, q_all: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
-             select: Sequence[int]) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+             select: Sequence[int], positions: Optional[torch.Tensor] = None,
+             q_weight: Optional[torch.Tensor] = None,
+             k_weight: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
         """One step for query block ``qb``: returns (OUT, LSE, per-partition weights).
 
         q_all, k, v are [B, S, H, D] for the whole sequence; the query block is
-        rows [offsets[qb], offsets[qb+1]) of q_all.
+        rows [offsets[qb], offsets[qb+1]) of q_all.  An engine with ``rotary``
+        takes the positions int32 [1 or B, S, axes] and, where it norms, the
+        weights of queries and keys.
         """
+        check_rotary_args(self.rotary, positions, q_weight, k_weight)
         c = self.cache(qb)
         a, e = self.offsets[qb], self.offsets[qb + 1]
         ws = self._attn_ws.get(q_all.dtype, self.B, self.H, self.D, e - a, self.offsets, select)
-        q, q0 = api.query_block(q_all, a, e - a)
+        if self.rotary is not None:
+            if qb not in self._rotated:
+                self._rotated[qb] = RotatedInputs(self.rotary, self.offsets, qb)
+            q, q0 = self._rotated[qb].begin(q_all, k, positions, q_weight, k_weight), 0
+            k = self._rotated[qb].keys(select)
+        else:
+            q, q0 = api.query_block(q_all, a, e - a)
         api.attn_block_states(q, q0, e - a, k, v, self.offsets, select, self.scale, c.out, c.lse, ws)
         for j, s in enumerate(select):
             if s:
