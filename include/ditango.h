@@ -366,7 +366,9 @@ size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk
  *   tensors      host, n_tensors (1 or 2: queries and keys of the same tokens)
  *                descriptions: x and y device, dtype `dt`, rows of D elements
  *                at the strides given (elements); y may be x (same strides),
- *                but may not overlap it otherwise.  weight device, dtype `dt`,
+ *                but may not overlap it otherwise, nor any row of an output
+ *                another (each stride passes what lies inside it), nor the other
+ *                tensor.  weight device, dtype `dt`,
  *                [D] (HEAD) or [heads][D] (ROW); unused without a norm.
  *                heads * D at most 65536.
  *   positions    device, int32 [pos_batches][S][n_axes], pos_batches 1 or B.

@@ -97,7 +97,7 @@ class ErrorModelSelectiveAttention:
         nws = max(api.norms_workspace_bytes(B, H, D, self.L, self.P), api.contrib_workspace_bytes(B, H, self.L, self.P))
         self._ws = torch.empty(max(16, nws), dtype=torch.uint8, device=device)
         self._attn_ws = AttnWorkspace(device)
-        self._rotated = RotatedInputs(rotary, self.offsets, q) if rotary is not None else None
+        self._rotated = RotatedInputs(rotary, self.offsets) if rotary is not None else None
 
     # ---------------------------------------------------------------- helpers
     def _norms(self, states: torch.Tensor, slots: Sequence[int], ref: Optional[torch.Tensor] = None) -> List[float]:
@@ -134,7 +134,7 @@ class ErrorModelSelectiveAttention:
         state actually carries) at every step after the first."""
         check_rotary_args(self._rotated, positions, q_weight, k_weight)
         if self._rotated is not None:
-            qb = self._rotated.begin(q_all, k, positions, q_weight, k_weight), 0
+            qb = self._rotated.begin(self.q, q_all, k, positions, q_weight, k_weight), 0
         else:
             qb = api.query_block(q_all, self.offsets[self.q], self.L)
         loc = [0] * self.P

@@ -54,7 +54,7 @@ INCLUDES = {"attn_bf16.hip": ["attn_tile.h", "attn_d128_loop.inc", "attn_d64_loo
             "cross.hip": ["attn_tile.h", "cross_tile.h"],
             "cross_few.hip": ["attn_tile.h", "cross_tile.h"],
             "cross_resident.hip": ["attn_tile.h", "cross_tile.h"],
-            "cross_task.hip": ["attn_tile.h", "cross_d128_loop.inc", "cross_d64_loop.inc"],
+            "cross_task.hip": ["attn_tile.h", "cross_tile.h", "cross_d128_loop.inc", "cross_d64_loop.inc"],
             "cross_f32.hip": ["attn_tile.h", "attn_f32_loop.h"],
             "rotary.hip": ["attn_tile.h"]}
 

@@ -37,6 +37,8 @@ class CrossAttention:
         key = (q.dtype, q.shape, k.shape, masked)
         n = self._bytes.get(key)
         if n is None:
+            if len(self._bytes) >= 4096:
+                self._bytes.clear()
             n = self._bytes[key] = api.cross_attn_workspace_bytes(
                 q.dtype, q.shape[0], q.shape[2], k.shape[2], q.shape[3], q.shape[1], k.shape[1], masked)
         if n == 0:
@@ -44,6 +46,7 @@ class CrossAttention:
         if self._ws is None or self._ws.numel() < n or self._ws.device != q.device:
             if self._ws is not None:
                 self._kept.append(self._ws)
+                n = max(n, 2 * self._ws.numel())     # what is kept stays below what is in use
             self._ws = torch.empty(n, dtype=torch.uint8, device=q.device)
         return self._ws
 

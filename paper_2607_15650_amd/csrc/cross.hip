@@ -24,8 +24,8 @@
 //
 // Rounding
 //   Products of bf16 values, accumulated in float32.  The probabilities go to
-//   bf16 for the second product (2^-9 of each; the row sum takes them before
-//   that), the output once more at its store.
+//   bf16 for the second product (by at most 2^-8 of each; the row sum takes them
+//   before that), the output once more at its store.
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -242,64 +242,66 @@ __global__ __launch_bounds__(256) void cross_pack_kernel(const CrossArgs a, int 
   if (tid == 0 && blockIdx.x == gridDim.x - 1) a.count[b] = to;
 }
 
-// Composes the partial states of a split launch: a wave per row, in the order
-// of the key ranges.  Bound by latency: lane p holds range p's weight (64
-// ranges at a time), and the ranges' rows are loaded in batches.
+// Composes the partial states of a split launch in the order of the key ranges:
+// D / 4 lanes per row, of 16 bytes each.  Lane p of a row holds range p's weight
+// (D / 4 ranges at a time), and the ranges' rows are loaded in batches.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
-  constexpr int E = D / 64, kBatch = 8;
-  typedef float VE __attribute__((ext_vector_type(E)));
+  constexpr int TEAM = D / 4;
   const int64_t rows = (int64_t)a.B * a.H * a.q_len;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (r >= rows) return;
-  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * (256 / TEAM) + threadIdx.x / TEAM;
+  const int64_t r = at < rows ? at : rows - 1;       // (a team past the end reads the last row)
+  const int lane = threadIdx.x & (TEAM - 1), first = threadIdx.x & 63 & ~(TEAM - 1);
   const int b = (int)(r / a.q_len / a.H);
   // ranges of fixed length behind the sequence's end have not been written
   const int parts = a.chunk > 0 ? min(a.split, (cross_keys(a, b) + a.chunk - 1) / a.chunk) : a.split;
   float mx = -INFINITY;
   bool bad = false;
-  for (int p = lane; p < parts; p += 64) {
+  for (int p = lane; p < parts; p += TEAM) {
     const float x = a.part_lse[p * rows + r];
     bad |= x != x;
     mx = fmaxf(mx, x);
   }
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-  bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+  for (int d = 1; d < TEAM; d <<= 1) {
+    mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+    bad |= __shfl_xor(bad ? 1 : 0, d, 64) != 0;
+  }
   const float mm = mx == -INFINITY ? 0.f : mx;
-  float tot = 0.f;
-  VE acc;
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-  for (int p0 = 0; p0 < parts; p0 += 64) {
+  float tot = 0.f, w;
+  f32x4 acc = f32x4{};
+  const float* src = a.part_out + r * D + lane * 4;
+  for (int p0 = 0; p0 < parts; p0 += TEAM) {
     const float mine = p0 + lane < parts ? a.part_lse[(p0 + lane) * rows + r] : -INFINITY;
-    const float w = fast_exp2((mine - mm) * 1.4426950408889634f);
+    w = fast_exp2((mine - mm) * 1.4426950408889634f);
     float sum = w;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d, 64);
+    for (int d = 1; d < TEAM; d <<= 1) sum += __shfl_xor(sum, d, 64);
     tot += sum;
-    const int np = min(parts - p0, 64);
-    for (int q0 = 0; q0 < np; q0 += kBatch) {
-      VE x[kBatch];
+    const int np = min(parts - p0, TEAM);
+    auto batch = [&](auto n, int q0) {
+      constexpr int N = decltype(n)::value;
+      f32x4 x[N];
 #pragma unroll
-      for (int q = 0; q < kBatch; ++q)
-        x[q] = *(const VE*)(a.part_out + ((p0 + min(q0 + q, np - 1)) * rows + r) * D + lane * E);
+      for (int q = 0; q < N; ++q) x[q] = *(const f32x4*)(src + (p0 + q0 + q) * rows * D);
 #pragma unroll
-      for (int q = 0; q < kBatch; ++q) {
-        // (past the last range the weight is left out, not 0 times a value)
-        if (q0 + q < np) {
-          const float wq = __shfl(w, q0 + q, 64);
+      for (int q = 0; q < N; ++q) {
+        const float wq = __shfl(w, first + q0 + q, 64);
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] = __builtin_fmaf(wq, x[q][e], acc[e]);
-        }
+        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wq, x[q][e], acc[e]);
       }
-    }
+    };
+    int q0 = 0;
+    for (; q0 + 8 <= np; q0 += 8) batch(std::integral_constant<int, 8>{}, q0);
+    if (np & 4) batch(std::integral_constant<int, 4>{}, q0), q0 += 4;
+    if (np & 2) batch(std::integral_constant<int, 2>{}, q0), q0 += 2;
+    if (np & 1) batch(std::integral_constant<int, 1>{}, q0);
   }
+  if (at >= rows) return;
   const float inv = tot > 0.f ? 1.0f / tot : bad ? NAN : 0.f;
   const int64_t tok = r % a.q_len, h = r / a.q_len % a.H;
-  T* dst = (T*)a.out + ((b * a.q_len + tok) * a.H + h) * D + lane * E;
-#pragma unroll
-  for (int e = 0; e < E; ++e) dst[e] = (T)(acc[e] * inv);
+  typedef T V __attribute__((ext_vector_type(4)));
+  *(V*)((T*)a.out + ((b * a.q_len + tok) * a.H + h) * D + lane * 4) = __builtin_convertvector(acc * inv, V);
   if (lane == 0 && a.lse != nullptr)
     a.lse[r] = tot > 0.f ? mx + __builtin_amdgcn_logf(tot) * kLn2 : bad ? NAN : -INFINITY;
 }
@@ -314,49 +316,48 @@ hipError_t launch_rows_cfg(const CrossArgs& a0, hipStream_t s) {
   CrossArgs a = a0;
   a.row_tiles = (a.rows + C::BM - 1) / C::BM;
   const int64_t grid = (int64_t)a.row_tiles * a.split * a.Hk * a.B;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!launch_fits(grid, C::NT)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((cross_kernel<C, WPE, LIST>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);
   return hipGetLastError();
 }
 template <int D, bool LIST>
 hipError_t launch_rows(const CrossArgs& a, hipStream_t s) {
-#ifdef SWEEP
-  const int cfg = getenv("RES") ? atoi(getenv("RES")) : 0;
-  if constexpr (!LIST) {
-  if (D == 64 && cfg == 1) return launch_rows_cfg<RowsCfg<D, 4>, 4, LIST>(a, s);
-  if (cfg == 2) return launch_rows_cfg<RowsCfg<D, 4>, 3, LIST>(a, s);
-  }
-#endif
   return launch_rows_cfg<RowsCfg<D, 4>, 2, LIST>(a, s);
 }
 
 // Estimated times in us of a launch of the two kernels that share a head's keys
-// between many rows, by how their workgroups fill the compute units, with the
-// split of the keys that is best for each (its join takes 4 us).  Measured (one
-// card): kRows a tile of 64 keys 1.4 us (D=64 0.9) where a compute unit has one
-// workgroup, 1.04 (0.53) for each where it has more, and 2.7 (1.3) beside them;
-// kTask 1.13 (0.97) a tile and 6.5 (4.9) a task.
+// between many rows, with the split of the keys that is best for each.  Fitted
+// to 70 shapes of one card (100 ... 20,000 rows x 4 ... 40 heads, 77 ... 4,096
+// keys; most lie within 10 %), D=64 in brackets:
+//  - kRows: w workgroups share a compute unit; a tile of 64 keys 0.96 w + 0.4
+//    (0.54 w + 0.25), and 3.2 w + 2 (1.5 w + 2.5) beside the tiles;
+//  - kTask: rounds of a task per compute unit, a tile 0.92 ... 1.42 (0.67 ...
+//    0.89) by how full the card is (its clock falls), 8 (5) beside a round's
+//    tiles and 3 once;
+//  - a split's partial states and their join 4, and 0.45 per MB: 2 x 4,095 rows
+//    x 12 heads against 2,048 keys 99 whole, 136 in two ranges; 300 x 40 against
+//    4,096 74 whole, 51 in three.
 struct Estimate {
   double us;
   int split;
 };
-Estimate estimate_rows(int64_t workgroups, int64_t tiles, int D, int cus) {
-  const double one = D == 128 ? 1.4 : 0.9, each = D == 128 ? 1.04 : 0.53, beside = D == 128 ? 2.7 : 1.3;
+double split_us(int64_t s, double state_mb) { return s > 1 ? 4 + 0.45 * (double)s * state_mb : 0; }
+Estimate estimate_rows(int64_t workgroups, int64_t tiles, int D, int cus, double state_mb) {
   Estimate best{1e30, 1};
   for (int64_t s = 1; s == 1 || (s <= tiles / 2 && s <= 64); ++s) {
     const double n = (double)(workgroups * s) / cus, w = n > 2 ? n : n > 1 ? 2 : 1;
-    const double tile = w * each > one ? w * each : one;
-    const double us = (double)((tiles + s - 1) / s) * tile + (w * beside > 2 ? w * beside : 2) + (s > 1 ? 4 : 0);
+    const double tile = D == 128 ? 0.96 * w + 0.4 : 0.54 * w + 0.25, beside = D == 128 ? 3.2 * w + 2 : 1.5 * w + 2.5;
+    const double us = (double)((tiles + s - 1) / s) * tile + beside + split_us(s, state_mb);
     if (us < best.us) best = {us, (int)s};
   }
   return best;
 }
-Estimate estimate_task(int64_t tasks, int64_t tiles, int D, int cus) {
-  const double tile = D == 128 ? 1.13 : 0.97, beside = D == 128 ? 6.5 : 4.9;
+Estimate estimate_task(int64_t tasks, int64_t tiles, int D, int cus, double state_mb) {
   Estimate best{1e30, 1};
   for (int64_t s = 1; s == 1 || (s <= tiles / 8 && s <= 16); ++s) {
-    const double rounds = (double)((tasks * s + cus - 1) / cus);
-    const double us = rounds * ((double)((tiles + s - 1) / s) * tile + beside) + (s > 1 ? 4 : 0);
+    const double rounds = (double)((tasks * s + cus - 1) / cus), full = (double)(tasks * s) / (rounds * cus);
+    const double tile = D == 128 ? 0.92 + 0.5 * full : 0.67 + 0.22 * full, beside = D == 128 ? 8 : 5;
+    const double us = rounds * ((double)((tiles + s - 1) / s) * tile + beside) + 3 + split_us(s, state_mb);
     if (us < best.us) best = {us, (int)s};
   }
   return best;
@@ -366,12 +367,12 @@ Estimate estimate_task(int64_t tasks, int64_t tiles, int D, int cus) {
 //  - kFew for up to 32 rows of a key/value head: 8 x 24 heads, 8 of them with
 //    keys, of one token against 16,384 keys 103 us (kRows 111), 12 heads against
 //    77 keys 4.7 us (5.4).
-//  - kResident where the keys fit LDS and every wave has two blocks of rows at
-//    least: 9,450 rows x 40 heads against 256 keys 65 us (kRows 78, kTask 83),
-//    14,850 x 48 at D=64 against 512 112 us (117, 137); but 2 x 4,095 x 12
-//    against 256 30 us (kRows 25).
-//  - kTask or kRows as estimated: 9,450 x 40 against 512 keys 112 us (kRows 119),
-//    against 1,024 178 us (210); 700 x 24 against 512 20 us (16).
+//  - kResident where the keys fit LDS and every wave of it has one and a half
+//    blocks of rows at least: 9,450 rows x 40 heads against 256 keys 68 us (kRows
+//    81, kTask 78), 20,000 x 8 against 256 33 (39, 41), 14,850 x 48 at D=64
+//    against 512 112 (117, 137); but 9,450 x 12 against 256 33 (30, 29).
+//  - kTask or kRows as estimated: 9,450 x 40 against 512 keys 113 us (kRows 125),
+//    against 1,024 183 (218); 700 x 24 against 512 19 (16).
 void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
   const int64_t heads = (int64_t)a.Hk * a.B, rows = a.rows, tiles = (a.kv_len + 63) / 64;
   if (rows <= 32) {
@@ -388,16 +389,18 @@ void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
     }
     return;
   }
-  if (a.kv_len <= cross_resident_keys(D) && (rows + 31) / 32 * heads >= 24 * (int64_t)cus) {
+  if (a.kv_len <= cross_resident_keys(D) &&
+      2 * ((rows + 31) / 32) * heads >= 3 * (int64_t)cross_resident_waves(D) * cus) {
     p->form = CrossPlan::kResident;
     return;
   }
-  const Estimate r = estimate_rows((rows + 127) / 128 * heads, tiles, D, cus);
+  const double state_mb = (double)a.B * a.H * a.q_len * D * 4e-6;
+  const Estimate r = estimate_rows((rows + 127) / 128 * heads, tiles, D, cus, state_mb);
   p->split = r.split;
   CrossArgs t = a;
   if (a.mask != nullptr) t.k_token = t.v_token = (int64_t)a.Hk * D;     // as packed
-  if (!cross_task_fits(t, D)) return;
-  Estimate k = estimate_task((rows + 255) / 256 * heads, tiles, D, cus);
+  if (!cross_task_fits(t, D) || (a.mask != nullptr && a.B > 65535)) return;   // (the packing's grid)
+  Estimate k = estimate_task((rows + 255) / 256 * heads, tiles, D, cus, state_mb);
   if (k.us < r.us) {
     p->form = CrossPlan::kTask;
     p->split = k.split;
@@ -487,7 +490,9 @@ hipError_t launch_cross(const CrossArgs& a0, const CrossPlan& p, ditango_dtype d
   else
     e = a.mask ? launch_rows<64, true>(a, s) : launch_rows<64, false>(a, s);
   if (e != hipSuccess || a.split == 1) return e;
-  const dim3 grid((unsigned)((rows + 3) / 4));
+  const int64_t per = 256 / (D / 4), join = ((int64_t)rows + per - 1) / per;
+  if (!launch_fits(join, 256)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)join);
   if (dt == DITANGO_F32 && D == 128) hipLaunchKernelGGL((cross_join_kernel<float, 128>), grid, dim3(256), 0, s, a);
   if (dt == DITANGO_F32 && D == 64) hipLaunchKernelGGL((cross_join_kernel<float, 64>), grid, dim3(256), 0, s, a);
   if (dt == DITANGO_BF16 && D == 128) hipLaunchKernelGGL((cross_join_kernel<__bf16, 128>), grid, dim3(256), 0, s, a);

@@ -196,7 +196,7 @@ hipError_t launch_few(const CrossArgs& a0, int dev, hipStream_t s) {
   CrossArgs a = a0;
   a.row_tiles = (a.rows + C::BM - 1) / C::BM;
   const int64_t grid = (int64_t)a.row_tiles * a.split * a.Hk * a.B;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!launch_fits(grid, C::NT)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((cross_few_kernel<C, LIST>), dim3((unsigned)grid), dim3(C::NT), C::LDS, s, a);
   return hipGetLastError();
 }

@@ -2,9 +2,9 @@
 // bf16 (gfx950): the keys and values of a head stay in LDS.
 //
 // A prompt's states of one head are small: 256 keys at D=64 take 64 KB.  A
-// workgroup of eight waves, one per compute unit, loads them once and its waves
-// walk over blocks of query rows by themselves, without a barrier: while one
-// wave of a SIMD takes exponentials the other's products run.  The next
+// workgroup per compute unit, of 12 waves (D=64: 16, as many as their registers
+// allow), loads them once and its waves walk over blocks of query rows by themselves, without a barrier: while one
+// wave of a SIMD takes exponentials the others' products run.  The next
 // block's queries are on their way from the last use of this one's on.
 #include <type_traits>
 
@@ -197,6 +197,7 @@ using Resident64 = ResidentCfg<64, 16>;
 }  // namespace
 
 int cross_resident_keys(int D) { return (D == 128 ? Resident128::MAX_TILES : Resident64::MAX_TILES) * 64; }
+int cross_resident_waves(int D) { return D == 128 ? Resident128::NW : Resident64::NW; }
 
 bool cross_resident_lists(const CrossArgs& a, int D) {
   const int64_t stride = a.k_token > a.v_token ? a.k_token : a.v_token;

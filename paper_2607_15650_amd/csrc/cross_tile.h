@@ -42,9 +42,6 @@ __device__ __forceinline__ void token_of(Args a, int row0, int r, int* tok, int*
   }
 }
 
-// s_waitcnt immediate: at most n vector-memory operations outstanding
-constexpr int vmcnt_imm(int n) { return (n & 15) | ((n >> 4) << 14) | 0x0F70; }
-
 // this wave's loads, into registers and into LDS, have landed
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -153,9 +150,11 @@ __device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], 
     float mx = sc[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-    const float mnew = fmaxf(m, pair_max(mx) * sl2);
+    // (-FLT_MAX where every score so far is -inf: their exponentials are zeros,
+    // those of any other score infinite, which raises m)
+    const float mnew = fmaxf(fmaxf(m, pair_max(mx) * sl2), -0x1.fffffep127f);
     if (!first) {
-      const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mnew);
+      const float alpha = fast_exp2(m - mnew);
       l *= alpha;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
@@ -163,14 +162,13 @@ __device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], 
     m = mnew;
   };
   auto probs = [&] {
-    const float mm = m == -INFINITY ? 0.f : m;
     sum = 0.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       f32x8 x;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        x[e] = fast_exp2(__builtin_fmaf(sc[8 * h + e], sl2, -mm));
+        x[e] = fast_exp2(__builtin_fmaf(sc[8 * h + e], sl2, -m));
         sum += x[e];
       }
       pf[h] = __builtin_convertvector(x, bf16x8);

@@ -346,6 +346,23 @@ bool aligned16(const void* p, const int64_t* strides, int64_t bytes) {
   return true;
 }
 
+// The rows of a rotary call's output do not overlap: from the closest ones on,
+// every stride passes what lies inside it.
+bool rows_apart(const ditango_rotary_tensor& t, int B, int64_t S, int D) {
+  const int64_t n[3] = {B, S, t.heads};
+  bool done[3] = {n[0] == 1, n[1] == 1, n[2] == 1};
+  int64_t extent = D;
+  for (;;) {
+    int k = -1;
+    for (int i = 0; i < 3; ++i)
+      if (!done[i] && (k < 0 || t.y_strides[i] < t.y_strides[k])) k = i;
+    if (k < 0) return true;
+    if (t.y_strides[k] < extent || t.y_strides[k] > INT64_MAX / 4 / n[k]) return false;
+    extent += t.y_strides[k] * (n[k] - 1);
+    done[k] = true;
+  }
+}
+
 // Argument checks of the cross attention that need the sizes only; fills them.
 ditango_status cross_sizes(ditango_dtype dt, int B, int H, int Hk, int D, int64_t q_len, int64_t kv_len, CrossArgs* a) {
   if (!valid_dtype(dt)) return DITANGO_ERR_INVALID;
@@ -406,7 +423,8 @@ ditango_status ditango_cross_attn(
   CrossPlan p;
   if (plan_cross(a, dt, D, &p) != hipSuccess) return DITANGO_ERR_HIP;
   if (workspace_bytes < p.need) return DITANGO_ERR_INVALID;
-  return from_hip(launch_cross(a, p, dt, D, workspace, workspace_bytes, (hipStream_t)stream));
+  const hipError_t e2 = launch_cross(a, p, dt, D, workspace, workspace_bytes, (hipStream_t)stream);
+  return e2 == hipErrorInvalidConfiguration ? DITANGO_ERR_UNSUPPORTED : from_hip(e2);
 }
 
 size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk, int D, int64_t q_len,
@@ -455,8 +473,13 @@ ditango_status ditango_rotary(
       // in place only where every element is read and written at one place
       if (t.x == t.y && t.x_strides[k] != t.y_strides[k]) return DITANGO_ERR_INVALID;
     }
+    if (!rows_apart(t, B, S, D)) return DITANGO_ERR_INVALID;
     a.t[i] = t;
   }
+  // (the first tensor's output is not what the second reads or writes)
+  if (n_tensors == 2 &&
+      (tensors[0].y == tensors[1].y || tensors[0].y == tensors[1].x || tensors[1].y == tensors[0].x))
+    return DITANGO_ERR_INVALID;
   for (int i = 0; i < rot_dim / 2; ++i) {
     if (!isfinite(freqs[i]) || axis[i] >= n_axes) return DITANGO_ERR_INVALID;
     a.turns[i] = freqs[i] * 0.15915494309189535;   // 1 / 2 pi
@@ -471,7 +494,8 @@ ditango_status ditango_rotary(
   a.pos_batch = pos_batches == 1 ? 0 : S * n_axes;
   a.factor = factor;
   a.eps = eps;
-  return from_hip(launch_rotary(a, dt, D, layout, norm, (hipStream_t)stream));
+  const hipError_t e = launch_rotary(a, dt, D, layout, norm, (hipStream_t)stream);
+  return e == hipErrorInvalidConfiguration ? DITANGO_ERR_UNSUPPORTED : from_hip(e);
 }
 
 ditango_status ditango_probe_mfma_bf16(int n_workgroups, int iters, float* sink, void* stream) {

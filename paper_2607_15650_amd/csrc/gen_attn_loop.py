@@ -488,6 +488,9 @@ def slow_block(g, par):
               f"v_max_f32 {v(TMP)}, {v(TMP)}, {v(TMP + 1)}",
               f"v_mul_f32 {v(TMP)}, {s_(S_SL2)}, {v(TMP)}",
               f"v_max_f32 {v(TMP)}, {v(M(qb))}, {v(TMP)}",          # m_new
+              # (task form: -FLT_MAX where every score so far is -inf, so that
+              # their exponentials are zeros, those of any other infinite)
+              *([f"v_max_f32 {v(TMP)}, 0xff7fffff, {v(TMP)}"] if g.task else []),
               f"v_sub_f32 {v(TMP + 2)}, {v(M(qb))}, {v(TMP)}",
               f"v_exp_f32 {v(TMP + 2)}, {v(TMP + 2)}",
               f"v_mov_b32 {v(TMP + 3)}, 0xff800000",

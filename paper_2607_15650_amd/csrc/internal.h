@@ -199,6 +199,11 @@ constexpr size_t kContribScratchBytes = DITANGO_CONTRIB_SCRATCH_BYTES;
 hipError_t contrib_scratch(float** ptr);
 hipError_t launch_norms(const NormArgs& a, ditango_dtype dt, hipStream_t s);
 
+// A launch has fewer than 2^31 workgroups and 2^32 threads.
+inline bool launch_fits(int64_t workgroups, int threads) {
+  return workgroups <= 0x7fffffff && workgroups * threads <= 0xffffffffLL;
+}
+
 // One launch of the cross attention.  The rows of a key/value head are those
 // of the query heads that share it: row r is token r / G of head hk * G + r % G.
 // Strides are in elements.
@@ -263,6 +268,7 @@ hipError_t launch_cross(const CrossArgs& a, const CrossPlan& p, ditango_dtype dt
 bool cross_task_fits(const CrossArgs& a, int D);
 hipError_t launch_cross_task(const CrossArgs& a, int D, hipStream_t s);
 int cross_resident_keys(int D);     // at most
+int cross_resident_waves(int D);    // of a workgroup, one per compute unit
 bool cross_resident_lists(const CrossArgs& a, int D);   // a masked call lists its live keys by itself
 hipError_t launch_cross_resident(const CrossArgs& a, int D, hipStream_t s);
 hipError_t launch_cross_few(const CrossArgs& a, int D, hipStream_t s);
@@ -288,7 +294,6 @@ struct RotaryArgs {
   double turns[DITANGO_ROTARY_MAX_PAIRS];    // of a pair, per position
   uint8_t axis[DITANGO_ROTARY_MAX_PAIRS];
 };
-// vec: elements of a load, as alignment and sizes allow
 hipError_t launch_rotary(const RotaryArgs& a, ditango_dtype dt, int D, ditango_rotary_layout layout,
                          ditango_rotary_norm norm, hipStream_t s);
 

@@ -253,6 +253,7 @@ hipError_t launch_vec(const RotaryArgs& a0, hipStream_t s) {
   }
   a.tokens = threads / a.team;
   const int64_t grid = ((int64_t)a.B * a.S + a.tokens - 1) / a.tokens;
+  if (!launch_fits(grid, threads)) return hipErrorInvalidConfiguration;
   const size_t lds = (size_t)a.tokens * (a.rot / 2) * sizeof(float2);
   hipLaunchKernelGGL((rotary_kernel<T, D, VEC, HALF, NORM>), dim3((unsigned)grid), dim3(threads), lds, s, a);
   return hipGetLastError();

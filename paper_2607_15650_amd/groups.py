@@ -81,7 +81,7 @@ class GroupedSelectiveAttention:
         self.groups = base_groups(self.P, q, g)
         self.computed_at = {grp: -1 for grp in self.groups}
         self._ws = None
-        self._rotated = RotatedInputs(rotary, self.offsets, q) if rotary is not None else None
+        self._rotated = RotatedInputs(rotary, self.offsets) if rotary is not None else None
 
     @property
     def state_bytes(self) -> int:
@@ -140,7 +140,7 @@ class GroupedSelectiveAttention:
         a = self.offsets[self.q]
         ws = self._attn_ws.get(q_all.dtype, self.B, self.H, self.D, self.L, self.offsets, sel)
         if self._rotated is not None:
-            q, q0 = self._rotated.begin(q_all, k, positions, q_weight, k_weight), 0
+            q, q0 = self._rotated.begin(self.q, q_all, k, positions, q_weight, k_weight), 0
             k = self._rotated.keys(sel)
         else:
             q, q0 = api.query_block(q_all, a, self.L)

@@ -119,38 +119,43 @@ class Rotary:
 
 
 class RotatedInputs:
-    """The rotated query block and keys of an engine's step, in buffers of its
-    own.  Only the rows that the step reads are rotated: the block, and the keys
-    of the partitions computed fresh (those of the block's own partition in the
-    same call as its queries)."""
+    """The rotated query block and keys of an engine's steps, in buffers of its
+    own that the steps share.  Only the rows that a step reads are rotated: the
+    block, and the keys of the partitions computed fresh (those of the block's
+    own partition in the same call as its queries)."""
 
-    def __init__(self, rotary: Rotary, offsets: Sequence[int], qb: int):
+    def __init__(self, rotary: Rotary, offsets: Sequence[int]):
         self.rotary = rotary
         self.offsets = [int(o) for o in offsets]
-        self.qb = qb
         self.q: Optional[torch.Tensor] = None
         self.k: Optional[torch.Tensor] = None
 
-    def begin(self, q_all: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
+    @staticmethod
+    def _buffer(old: Optional[torch.Tensor], like: torch.Tensor) -> torch.Tensor:
+        """Room for a dense ``like``: the old one where it fits."""
+        if old is None or old.numel() < like.numel() or old.dtype != like.dtype or old.device != like.device:
+            return like.new_empty(like.numel())
+        return old
+
+    def begin(self, qb: int, q_all: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
               q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor]) -> torch.Tensor:
-        """Starts a step with its tensors ([B, S, H, D], positions [1 or B, S,
-        axes]): returns the rotated query block [B, L, H, D].  The block's own
-        keys are rotated with it."""
-        a, e = self.offsets[self.qb], self.offsets[self.qb + 1]
+        """Starts a step of query block ``qb`` with its tensors ([B, S, H, D],
+        positions [1 or B, S, axes]): returns the rotated block [B, L, H, D].
+        The block's own keys are rotated with it."""
+        a, e = self.offsets[qb], self.offsets[qb + 1]
         if positions is None or positions.dim() != 3 or positions.shape[1] != k.shape[1] or \
                 k.shape[1] != self.offsets[-1]:
             raise ValueError("an engine with rotary positions needs positions [1 or B, S, axes] of the whole sequence")
-        B, H, D = q_all.shape[0], q_all.shape[2], q_all.shape[3]
-        if self.q is None or self.q.shape != (B, e - a, H, D) or self.q.dtype != q_all.dtype or self.q.device != q_all.device:
-            self.q = q_all.new_empty((B, e - a, H, D))
-        if self.k is None or self.k.shape != k.shape or self.k.dtype != k.dtype or self.k.device != k.device:
-            self.k = k.new_empty(k.shape)
+        block = q_all[:, a:e]
+        self.q = self._buffer(self.q, block)
+        self.k = self._buffer(self.k, k)
+        q = self.q[:block.numel()].view(block.shape)
+        self._k = self.k[:k.numel()].view(k.shape)
         self._src, self._pos, self._kw = k, positions, k_weight
-        self._done = {self.qb}
+        self._done = {qb}
         if e > a:
-            self.rotary(q_all[:, a:e], k[:, a:e], positions[:, a:e].contiguous(), q_weight, k_weight, self.q,
-                        self.k[:, a:e])
-        return self.q
+            self.rotary(block, k[:, a:e], positions[:, a:e].contiguous(), q_weight, k_weight, q, self._k[:, a:e])
+        return q
 
     def keys(self, select: Sequence[int]) -> torch.Tensor:
         """K [B, S, H, D] with the rows of the selected partitions rotated."""
@@ -166,8 +171,8 @@ class RotatedInputs:
                 j += 1
             a, e = self.offsets[i], self.offsets[j]
             if e > a:
-                self.rotary(self._src[:, a:e], None, self._pos[:, a:e].contiguous(), self._kw, q_out=self.k[:, a:e])
-        return self.k
+                self.rotary(self._src[:, a:e], None, self._pos[:, a:e].contiguous(), self._kw, q_out=self._k[:, a:e])
+        return self._k
 
 
 def check_rotary_args(rotary: Optional[Rotary], positions, q_weight, k_weight) -> None:

@@ -39,7 +39,7 @@ class SelectiveAttention:
     With ``rotary`` the steps take queries and keys as the projections leave
     them, and their positions (``rotary.Rotary``: the norm of queries and keys
     and their rotation); a step then rotates the query block and the keys of the
-    partitions it computes fresh, into buffers kept for the query block.
+    partitions it computes fresh, into buffers that the steps share.
 
     The steps of one instance share its workspaces, whatever the query block:
     order them on one stream, or across streams by events.
@@ -57,7 +57,7 @@ class SelectiveAttention:
         self.device = device
         self.caches = {}
         self.rotary = rotary
-        self._rotated = {}
+        self._rotated = RotatedInputs(rotary, self.offsets) if rotary is not None else None
         self._ws = {}
         self._attn_ws = AttnWorkspace(device)
 
@@ -83,10 +83,8 @@ class SelectiveAttention:
         a, e = self.offsets[qb], self.offsets[qb + 1]
         ws = self._attn_ws.get(q_all.dtype, self.B, self.H, self.D, e - a, self.offsets, select)
         if self.rotary is not None:
-            if qb not in self._rotated:
-                self._rotated[qb] = RotatedInputs(self.rotary, self.offsets, qb)
-            q, q0 = self._rotated[qb].begin(q_all, k, positions, q_weight, k_weight), 0
-            k = self._rotated[qb].keys(select)
+            q, q0 = self._rotated.begin(qb, q_all, k, positions, q_weight, k_weight), 0
+            k = self._rotated.keys(select)
         else:
             q, q0 = api.query_block(q_all, a, e - a)
         api.attn_block_states(q, q0, e - a, k, v, self.offsets, select, self.scale, c.out, c.lse, ws)

@@ -257,6 +257,75 @@ def test_scores_of_any_size(gpu_lib, dtype, Lq):
     assert float((out.double().cpu() - eo).abs().max()) <= ((2 ** -7 + 1e-3) if dtype == BF16 else 1e-3) * vm
 
 
+# the kernels for a token, for few rows, for a head's keys in LDS and for many rows and keys
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Lq,S,H", [(1, 200, 2), (1, 5000, 2), (200, 333, 2), (4500, 200, 48), (2500, 900, 24)])
+def test_scores_of_minus_infinity(gpu_lib, dtype, D, Lq, S, H):
+    """Keys whose every score is -inf, the first of all among them, weigh nothing beside others."""
+    from paper_2607_15650_amd.cross import CrossAttention
+    q, k, v = make(1, Lq, S, H, H, D, dtype, seed=8)
+    q[..., 0] = q[..., 0].abs() + 0.125
+    live = torch.ones(1, S, dtype=torch.bool, device="cuda")
+    live[:, :170] = False
+    live[:, 180:190] = False
+    k[..., 0] = torch.where(live[:, :, None], k[..., 0], -math.inf)
+    # (exponents far below the others' too: nothing else may stand for the maximum)
+    q[..., 1] = q[..., 1].abs() + 0.125
+    k[..., 1] = -200.0
+    out, lse = CrossAttention(D ** -0.5)(q, k, v)
+    eo, el = exact(q, k, v, D ** -0.5, live, "cuda")
+    vm = float(v.abs().max())
+    # scores of up to 100, off by 2^-24 * 8 of that
+    assert float((lse.double().cpu() - el).abs().max()) <= 1e-4
+    assert float((out.double().cpu() - eo).abs().max()) <= ((2 ** -7 + 2e-4) if dtype == BF16 else 2e-4) * vm
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("Lq,H,far", [(1, 2, False), (150, 2, False), (150, 2, True), (4500, 48, False)])
+@pytest.mark.parametrize("masked", [False, True])
+def test_rows_far_apart(gpu_lib, dtype, Lq, H, far, masked):
+    """Offsets past 2^31 elements: keys and values, and the queries, as columns of wide rows."""
+    from paper_2607_15650_amd import api
+    S, D, wide = 270, 64, 1 << 23
+
+    def column(n, at, wide):
+        x = torch.as_strided(buf, (1, n, H, D), (0, wide, D, 1), at)
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        return x
+
+    buf = torch.empty(S * wide, dtype=dtype, device="cuda")
+    k, v = column(S, 0, wide), column(S, H * D, wide)
+    if far:
+        q = column(Lq, 2 * H * D, wide)
+    else:
+        q = torch.randn(1, Lq, H, D, device="cuda").to(dtype)
+    mask = (torch.rand(1, S, device="cuda") < 0.6) if masked else None
+    live = mask if masked else torch.ones(1, S, dtype=torch.bool, device="cuda")
+    ws = torch.empty(api.cross_attn_workspace_bytes(dtype, 1, H, H, D, Lq, S, masked), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty(1, Lq, H, D, dtype=dtype, device="cuda"), torch.empty(1, H, Lq, device="cuda")
+    api.cross_attn(q, k, v, 0.125, out, lse, None, mask, ws)
+    check((out, lse), q, k, v, 0.125, live, "cuda")
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_many_sequences(gpu_lib, masked):
+    """More sequences than a grid's second dimension holds; more threads than a launch has are refused."""
+    from paper_2607_15650_amd import _lib, api
+    from paper_2607_15650_amd.cross import CrossAttention
+    B, Lq, S, D = 66000, 40, 600, 64
+    q, (k, v) = torch.randn(B, Lq, 1, D, device="cuda").to(BF16), torch.randn(2, 1, S, 1, D, device="cuda").to(BF16)
+    mask = (torch.rand(B, S, device="cuda") < 0.5) if masked else None
+    out, lse = CrossAttention(0.125)(q, k.expand(B, S, 1, D), v.expand(B, S, 1, D), key_mask=mask)
+    at = torch.tensor([0, 1, 65534, 65535, 65536, B - 1], device="cuda")
+    live = mask[at] if masked else torch.ones(6, S, dtype=torch.bool, device="cuda")
+    check((out[at], lse[at]), q[at], k.expand(6, S, 1, D), v.expand(6, S, 1, D), 0.125, live)
+    B = 1 << 24
+    q = torch.zeros(1, 1, 1, D, dtype=BF16, device="cuda").expand(B, 1, 1, D)
+    with pytest.raises(_lib.DitangoError):
+        api.cross_attn(q, q, q, 0.125, torch.empty(B, 1, 1, D, dtype=BF16, device="cuda"))
+
+
 def test_composes_with_other_states(gpu_lib):
     """A state like the partitions': the halves of the keys, composed, are the whole."""
     from paper_2607_15650_amd import api

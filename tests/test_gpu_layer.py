@@ -111,7 +111,7 @@ def test_layer(gpu_lib, graph):
     else:
         got = layer()
     live = torch.arange(77, device="cuda") < lens[:, None]
-    qr, kr = engine._rotated[0].q, engine._rotated[0].k
+    qr, kr = op(q[:, :OFFS[1]].contiguous(), None, pos[:, :OFFS[1]].contiguous(), wq), op(k, None, pos, wk)
     # the probabilities' and the output's rounding, and that of the states that are composed: 2^-8 each of at most
     # max|v|; float32 accumulation beside them
     tol = lambda t: (3 * 2.0 ** -8 + 2.0 ** -16) * float(t.abs().max())   # noqa: E731

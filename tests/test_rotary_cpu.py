@@ -149,3 +149,10 @@ def test_rotary_refusals(L):
     assert rotary(L, xs=(-384, 128, 64)) == 1
     assert rotary(L, xs=(768, 256, 64)) == 1   # in place with other strides
     assert rotary(L, B=1 << 16, S=1 << 16) == 2
+    # outputs whose rows overlap: repeated, closer than a row, interleaved heads; two tensors at one place
+    other = ctypes.create_string_buffer(16)
+    for ys in ((768, 128, 0), (0, 128, 64), (768, 64, 64), (768, 128, 32), (64, 128, 64)):
+        assert rotary(L, B=2, heads=2, y=ctypes.addressof(other), ys=ys) == 1
+    assert rotary(L, n=2) == 1
+    # 2^32 threads: a launch has fewer
+    assert rotary(L, S=1 << 30, heads=1) == 2
