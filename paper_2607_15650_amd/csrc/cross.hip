@@ -329,10 +329,10 @@ hipError_t launch_rows(const CrossArgs& a, hipStream_t s) {
 // between many rows, with the split of the keys that is best for each.  Fitted
 // to 70 shapes of one card (100 ... 20,000 rows x 4 ... 40 heads, 77 ... 4,096
 // keys; most lie within 10 %), D=64 in brackets:
-//  - kRows: w workgroups share a compute unit; a tile of 64 keys 0.96 w + 0.4
+//  - kRows: w workgroups share a compute unit; a tile of 64 keys 0.96 w + 0.45
 //    (0.54 w + 0.25), and 3.2 w + 2 (1.5 w + 2.5) beside the tiles;
-//  - kTask: rounds of a task per compute unit, a tile 0.92 ... 1.42 (0.67 ...
-//    0.89) by how full the card is (its clock falls), 8 (5) beside a round's
+//  - kTask: rounds of a task per compute unit, a tile 0.9 ... 1.4 (0.67 ...
+//    0.89) by how full the card is (its clock falls), 7.25 (5) beside a round's
 //    tiles and 3 once;
 //  - a split's partial states and their join 4, and 0.45 per MB: 2 x 4,095 rows
 //    x 12 heads against 2,048 keys 99 whole, 136 in two ranges; 300 x 40 against
@@ -345,8 +345,8 @@ double split_us(int64_t s, double state_mb) { return s > 1 ? 4 + 0.45 * (double)
 Estimate estimate_rows(int64_t workgroups, int64_t tiles, int D, int cus, double state_mb) {
   Estimate best{1e30, 1};
   for (int64_t s = 1; s == 1 || (s <= tiles / 2 && s <= 64); ++s) {
-    const double n = (double)(workgroups * s) / cus, w = n > 2 ? n : n > 1 ? 2 : 1;
-    const double tile = D == 128 ? 0.96 * w + 0.4 : 0.54 * w + 0.25, beside = D == 128 ? 3.2 * w + 2 : 1.5 * w + 2.5;
+    const double n = (double)(workgroups * s) / cus, w = n > 2 ? n : n > 1 ? (n + 2) / 2 : 1;
+    const double tile = D == 128 ? 0.96 * w + 0.45 : 0.54 * w + 0.25, beside = D == 128 ? 3.2 * w + 2 : 1.5 * w + 2.5;
     const double us = (double)((tiles + s - 1) / s) * tile + beside + split_us(s, state_mb);
     if (us < best.us) best = {us, (int)s};
   }
@@ -356,7 +356,7 @@ Estimate estimate_task(int64_t tasks, int64_t tiles, int D, int cus, double stat
   Estimate best{1e30, 1};
   for (int64_t s = 1; s == 1 || (s <= tiles / 8 && s <= 16); ++s) {
     const double rounds = (double)((tasks * s + cus - 1) / cus), full = (double)(tasks * s) / (rounds * cus);
-    const double tile = D == 128 ? 0.92 + 0.5 * full : 0.67 + 0.22 * full, beside = D == 128 ? 8 : 5;
+    const double tile = D == 128 ? 0.9 + 0.5 * full : 0.67 + 0.22 * full, beside = D == 128 ? 7.25 : 5;
     const double us = rounds * ((double)((tiles + s - 1) / s) * tile + beside) + 3 + split_us(s, state_mb);
     if (us < best.us) best = {us, (int)s};
   }
