@@ -26,6 +26,8 @@
 //   Products of bf16 values, accumulated in float32.  The probabilities go to
 //   bf16 for the second product (by at most 2^-8 of each; the row sum takes them
 //   before that), the output once more at its store.
+#include <math.h>
+
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -378,11 +380,17 @@ void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
   if (rows <= 32) {
     p->form = CrossPlan::kFew;
     if (a.kv_len > 768) {
-      // four workgroups for a compute unit, of 256 keys at least (the join
-      // takes as long as 600 keys)
+      // four workgroups for a compute unit, of 256 keys at least.  Where fewer
+      // keys leave compute units idle a key of a range takes 7 ns and a range
+      // 90 ns in the join: least together at sqrt(12.5 kv_len) keys (a token of
+      // 8 heads on one head's 100,000 keys: 256 a range 42 us, 1,152 23 us;
+      // 6 on 40,000: 25 us, 768 18 us)
       const int64_t want = (4 * (int64_t)cus + heads - 1) / heads;
-      const int64_t chunk = ((a.kv_len + want - 1) / want + 127) / 128 * 128;
-      p->chunk = (int)(chunk > 256 ? chunk : 256);
+      int64_t chunk = (a.kv_len + want - 1) / want;
+      const int64_t least = (int64_t)sqrt(12.5 * a.kv_len);
+      if (chunk < least) chunk = least;
+      if (chunk < 256) chunk = 256;
+      p->chunk = (int)((chunk + 127) / 128 * 128);
       p->split = (a.kv_len + p->chunk - 1) / p->chunk;
     } else {
       p->chunk = a.kv_len;
