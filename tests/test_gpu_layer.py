@@ -120,6 +120,27 @@ def test_layer(gpu_lib, graph):
     assert float((y.double().cpu() - attention64(x, text_k, text_v, scale, live)).abs().max()) <= tol(text_v)
 
 
+def test_a_captured_step_keeps_its_buffers(gpu_lib):
+    """Steps of larger query blocks, after the capture of a smaller one's, leave its replays as they were."""
+    from paper_2607_15650_amd.step import SelectiveAttention
+    pos, scale = positions(), D ** -0.5
+    q, k, v, wq, wk = inputs(7)
+    engine, other = (SelectiveAttention(B, H, D, OFFS, scale, rotary=rotary()) for _ in range(2))
+    engine.step(0, 1, q, k, v, [1] * P, pos, wq, wk)           # 140 rows, of at most 230
+    torch.cuda.synchronize()
+    rec = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(rec):
+        got = engine.step(0, 1, q, k, v, [1] * P, pos, wq, wk)
+    for i in range(3):
+        engine.step(0, 3, q, k, v, [1] * P, pos, wq, wk)
+        fill = [torch.full((B, 230, H, D), math.nan, dtype=BF16, device="cuda") for _ in range(8)]
+        q.copy_(torch.randn(q.shape, device="cuda"))
+        rec.replay()
+        want = other.step(0, 1, q, k, v, [1] * P, pos, wq, wk)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool(torch.isnan(torch.stack(fill)).all())
+
+
 def test_refusals(gpu_lib):
     from paper_2607_15650_amd.step import SelectiveAttention
     q, k, v, wq, wk = inputs(1)
