@@ -326,7 +326,8 @@ ditango_status ditango_state_norms(
  *                kv_lens[b] (clamped to 0 ... kv_len); null: all.
  *   key_mask     device, [B][kv_len] bytes, non-zero = live; null: all.  With
  *                kv_lens both hold.
- *   out          device, [B][q_len][H][D] in dtype `dt`, 16-byte aligned.
+ *   out          device, [B][q_len][H][D] in dtype `dt`, 16-byte aligned; may not
+ *                overlap the inputs.
  *   lse          device, [B][H][q_len] float32, or null.
  *   workspace    device, 256-byte aligned, ditango_cross_attn_workspace_bytes
  *                bytes; contents do not matter before or after.  A call with

@@ -405,6 +405,7 @@ ditango_status ditango_cross_attn(
     return DITANGO_ERR_UNSUPPORTED;
   // offsets inside a tile of keys are 32 bits
   if (k_strides[1] >= (1 << 24) || v_strides[1] >= (1 << 24)) return DITANGO_ERR_UNSUPPORTED;
+  if (out == q || out == k || out == v) return DITANGO_ERR_INVALID;   // (rows are read again after others are written)
   if (((uintptr_t)workspace & 255u) != 0) return DITANGO_ERR_INVALID;
   a.q = q;
   a.k = k;

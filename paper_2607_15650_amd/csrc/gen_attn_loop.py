@@ -3,7 +3,7 @@ attention kernel at head dim 128 and 64 as one block of gfx950 assembly
 each, scheduled by hand; and cross_d128_loop.inc and cross_d64_loop.inc, the
 same loop for workgroups that run one task after another (the cross
 attention's): Q^T comes in registers, the first tiles are in the ring, and the
-next task's Q^T is loaded into other registers while the last two key tiles
+next task's Q^T is loaded into other registers while the last three key tiles
 are worked on.
 
 The loop computes, for one task (256 query rows of one head against the keys

@@ -63,7 +63,7 @@ def test_grid_positions():
 
 
 def cross(L, q=FAKE, k=FAKE, v=FAKE, dt=1, B=2, H=4, Hk=2, D=64, q_len=3, kv_len=5, qs=None, ks=None, vs=None,
-          lens=None, mask=None, scale=0.1, out=FAKE, lse=FAKE, ws=None, n=0):
+          lens=None, mask=None, scale=0.1, out=FAKE + 4096, lse=FAKE, ws=None, n=0):
     I3 = ctypes.c_int64 * 3
     qs = qs or (q_len * H * D, H * D, D)
     ks = ks or (kv_len * Hk * D, Hk * D, D)
@@ -98,6 +98,9 @@ def test_cross_refusals(L):
     assert cross(L, ks=(640, 132, 64)) == 2
     assert cross(L, vs=(640, 128, 60)) == 2
     assert cross(L, ks=(1 << 40, 1 << 24, 64)) == 2
+    # the output at an input's place
+    for kw in (dict(k=FAKE + 256, v=FAKE + 512), dict(q=FAKE + 256, v=FAKE + 512), dict(q=FAKE + 256, k=FAKE + 512)):
+        assert cross(L, out=FAKE, **kw) == 1
     # a mask needs a workspace, 256-byte aligned and large enough
     assert cross(L, mask=FAKE) == 1
     assert cross(L, mask=FAKE, ws=FAKE, n=100) == 1
