@@ -48,27 +48,29 @@ def _dev(*ts: torch.Tensor) -> None:
         raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
 
 
-def _dev_strided(strided: Sequence[torch.Tensor], dense: Sequence[Optional[torch.Tensor]]) -> None:
+def _dev_strided(strided: Sequence[torch.Tensor], dense: Sequence[Optional[torch.Tensor]]) -> int:
     """_dev for tensors whose rows lie apart (only their last dim is dense),
-    together with dense ones."""
-    dev = strided[0].device
+    together with dense ones; returns the device."""
+    # (by number: -1 for the CPU's; a device object takes 0.1 us a tensor more)
+    dev = strided[0].get_device()
     # the kernels are enqueued on the current device's current stream
-    if dev.type != "cuda":
+    if dev < 0 or not strided[0].is_cuda:
         raise ValueError("all tensors must be on the GPU")
-    if dev.index != torch._C._cuda_getDevice():
+    if dev != torch._C._cuda_getDevice():
         raise ValueError("tensors must be on the current device (torch.cuda.set_device)")
     for t in strided:
-        if t.device != dev:
+        if t.get_device() != dev:
             raise ValueError("all tensors must be on one device")
         if t.stride(-1) != 1 and t.shape[-1] > 1:
             raise ValueError("the elements of a row must be contiguous")
     for t in dense:
         if t is None:
             continue
-        if t.device != dev:
+        if t.get_device() != dev:
             raise ValueError("all tensors must be on one device")
         if not t.is_contiguous():
             raise ValueError("all tensors must be contiguous")
+    return dev
 
 
 # strides of [B, tokens, heads] as the C ABI takes them
@@ -340,7 +342,7 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, 
     query block with it."""
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q, k and v must be [B, tokens, heads, D]")
-    _dev_strided((q, k, v), (out, lse, kv_lens, key_mask, workspace))
+    dev = _dev_strided((q, k, v), (out, lse, kv_lens, key_mask, workspace))
     B, q_len, H, D = q.shape
     Bk, kv_len, Hk, Dk = k.shape
     if k.shape != v.shape or Bk != B or Dk != D:
@@ -367,7 +369,8 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, 
         q.data_ptr(), _strides(*q.stride()), k.data_ptr(), _strides(*k.stride()), v.data_ptr(), _strides(*v.stride()),
         _dtype(q), B, H, Hk, D, q_len, kv_len,
         kv_lens.data_ptr() if kv_lens is not None else None, key_mask.data_ptr() if key_mask is not None else None,
-        float(scale), out.data_ptr(), lse.data_ptr() if lse is not None else None, ws, n, _stream())
+        scale, out.data_ptr(), lse.data_ptr() if lse is not None else None, ws, n,
+        torch._C._cuda_getCurrentRawStream(dev))
     _lib.check("ditango_cross_attn", st)
 
 
@@ -376,6 +379,9 @@ def rotary_tables(freqs: Sequence[float], axis: Sequence[int]):
     if len(freqs) != len(axis):
         raise ValueError("freqs and axis must have one entry per pair")
     return (ctypes.c_double * len(freqs))(*freqs), (ctypes.c_uint8 * len(axis))(*axis)
+
+
+_ROTARY_TENSORS = (None, _lib.RotaryTensor * 1, _lib.RotaryTensor * 2)
 
 
 def rotary(xs: Sequence[torch.Tensor], ys: Sequence[torch.Tensor], positions: torch.Tensor, tables, rot_dim: int,
@@ -392,7 +398,7 @@ def rotary(xs: Sequence[torch.Tensor], ys: Sequence[torch.Tensor], positions: to
     x0 = xs[0]
     if x0.dim() != 4:
         raise ValueError("tensors must be [B, S, heads, D] of the same tokens, outputs like them")
-    _dev_strided((*xs, *ys), (positions, *weights[:n]))
+    dev = _dev_strided((*xs, *ys), (positions, *weights[:n]))
     B, S, _, D = x0.shape
     dt = x0.dtype
     if positions.dtype != torch.int32 or positions.dim() != 3 or positions.shape[1] != S or \
@@ -400,7 +406,7 @@ def rotary(xs: Sequence[torch.Tensor], ys: Sequence[torch.Tensor], positions: to
         raise ValueError("positions must be int32 [1 or B, S, axes]")
     if len(tables[0]) * 2 != rot_dim:
         raise ValueError("the tables must have one entry per pair of rot_dim")
-    arr = (_lib.RotaryTensor * n)()
+    arr = _ROTARY_TENSORS[n]()
     for a, x, y, w in zip(arr, xs, ys, weights):
         if x.dim() != 4 or x.shape[0] != B or x.shape[1] != S or x.shape[3] != D or y.shape != x.shape:
             raise ValueError("tensors must be [B, S, heads, D] of the same tokens, outputs like them")
@@ -416,7 +422,7 @@ def rotary(xs: Sequence[torch.Tensor], ys: Sequence[torch.Tensor], positions: to
         a.x_strides, a.y_strides = _strides(*x.stride()), _strides(*y.stride())
     st = _lib.lib().ditango_rotary(
         arr, n, _dtype(x0), B, S, D, positions.data_ptr(), positions.shape[0], positions.shape[2],
-        tables[0], tables[1], rot_dim, layout, factor, norm, eps, _stream())
+        tables[0], tables[1], rot_dim, layout, factor, norm, eps, torch._C._cuda_getCurrentRawStream(dev))
     _lib.check("ditango_rotary", st)
 
 
