@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
     // the loop over the keys; `checked` tests every tile for the maximum
     auto key_loop = [&](auto checked) {
       a = args();
-      // (without keys: one tile of zeros, whose sum is dropped below)
+      // (without keys: one tile of zeros, whose sum and products are dropped below)
       const uint32_t ntiles = (uint32_t)((max(n, 1) + C::BN - 1) / C::BN), kvl = (uint32_t)n;
       const float sl2 = a->scale_log2;
       if constexpr (D == 128) {
@@ -297,6 +297,13 @@ asm volatile(BODY                                                               
     first_tiles(a, next, key0, n, &kd, &vd);
     lane = lane_id();
     lr = lane & 31, g = lane >> 5;
+    // (without keys the tile of zeros leaves NaN where a query is no number)
+    if (!keys) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[qb][db] = f32x16{};
+    }
 
     if (a->split > 1) {
       // ---- the partial state of a key range, as it lies in the registers
