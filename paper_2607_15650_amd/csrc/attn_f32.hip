@@ -21,10 +21,10 @@
 //   have an accumulator of their own.
 //   What the planes cannot hold goes through the float32 MFMA: a workgroup
 //   runs its task again with it
-//    - where some row's sum or output ends up not finite.  A value that is not
-//      finite, or rounds to infinity in bf16, gives NaN in the planes and in
-//      every row it enters; the float32 MFMA treats infinities as float32
-//      arithmetic does;
+//    - where some row's sum or output ends up not finite, or beyond 2^120
+//      (state_out_of_range).  A value that is not finite, or rounds to infinity
+//      in bf16, gives NaN in the planes and in every row it enters; the float32
+//      MFMA treats infinities as float32 arithmetic does;
 //    - where nonzero values below 2^-110 matter.  Their third plane falls
 //      under bf16's smallest subnormal (2^-133), so such a value is off by up
 //      to 2^-134.  Its queries are looked at as they are split: one of these
@@ -94,31 +94,31 @@ __global__ __launch_bounds__(C::NT, C::WPE) void attn_f32_kernel(const AttnArgs 
   const int gt = C::KW == 1 ? tid : lane;
   float* part_m = (float*)(smem + C::KW * C::GROUP);         // [KW][32] maximum, then [KW][32] row sum
   float* part_l = part_m + C::KW * 32;
-  // run the task again; look through V; V asks for it (a word each: a wave may
-  // still be reading one when another writes the next)
+  // run the task again; look through V; V asks for it; run it again for a state
+  // out of range (a word each: a wave may still be reading one when another
+  // writes the next)
   int* redo = (int*)(part_l + C::KW * 32);
 
   f32x16 o[C::DB];
   float m, l;
-  if (tid < 3) redo[tid] = 0;
+  if (tid < 4) redo[tid] = 0;
   uint64_t ask = 0;
   key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
-  // sum of 0 * x: NaN where a value is not finite
-  float bad = l * 0.f, low = INFINITY;
+  const bool range = t0 < t1 && state_out_of_range(o, l);
+  float small_o = INFINITY;
 #pragma unroll
   for (int db = 0; db < C::DB; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      bad = __builtin_fmaf(o[db][r], 0.f, bad);
-      low = fminf(low, fabsf(o[db][r]));
-    }
+    for (int r = 0; r < 16; ++r) small_o = fminf(small_o, fabsf(o[db][r]));
   const float below = pair_sum(l) * 0x1p-100f;
-  const bool small = row_ok && low < below;
+  const bool small = row_ok && small_o < below;
   __syncthreads();
-  if ((__builtin_amdgcn_ballot_w64(!(bad == 0.f)) | ask) != 0 && lane == 0) redo[0] = 1;
+  if (ask != 0 && lane == 0) redo[0] = 1;
+  if (__builtin_amdgcn_ballot_w64(range) != 0 && lane == 0) redo[3] = 1;
   if (__builtin_amdgcn_ballot_w64(small) != 0 && lane == 0) redo[1] = 1;
   __syncthreads();
-  bool again = __builtin_amdgcn_readfirstlane(redo[0]) != 0;
+  const bool far = __builtin_amdgcn_readfirstlane(redo[3]) != 0;
+  bool again = far || __builtin_amdgcn_readfirstlane(redo[0]) != 0;
   if (!again && __builtin_amdgcn_readfirstlane(redo[1]) != 0) {
     constexpr int kBatch = 8;                                // loads in flight
     const int64_t units = (int64_t)kv_len * (D / 4);
@@ -140,7 +140,8 @@ __global__ __launch_bounds__(C::NT, C::WPE) void attn_f32_kernel(const AttnArgs 
     again = __builtin_amdgcn_readfirstlane(redo[2]) != 0;
   }
   if (again) {
-    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
+    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask,
+                       far ? wide_low(kv_len) : 0.f);
     __syncthreads();
   }
 

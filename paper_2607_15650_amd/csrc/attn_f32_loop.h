@@ -99,13 +99,15 @@ struct ListedRows {
 
 // One pass over this wave's (KW > 1) or workgroup's (KW = 1) key tiles
 // [t0, t1): unnormalised O^T, row maximum m (base 2, scaled) and the lane's
-// half of the row sum.  SPLIT: bf16 planes, otherwise the float32 MFMA.
+// half of the row sum.  SPLIT: bf16 planes, otherwise the float32 MFMA, which
+// takes the probabilities as 2^low exp2(scale (s - max)) against the maximum as
+// it is (attn_tile.h; low 0 but for rows out of range).
 // `ask`: the lanes whose query values need the latter.
 template <class C, bool SPLIT, class Rows>
 __device__ __forceinline__ void key_loop(const float* __restrict__ qrow, bool row_ok, const Rows& kg,
                                          const Rows& vg, int kv_len, int t0, int t1,
                                          float sl2, unsigned char* buf, int gt, f32x16 (&o)[C::DB],
-                                         float& m, float& l, uint64_t& ask) {
+                                         float& m, float& l, uint64_t& ask, float low = 0.f) {
   constexpr int D = C::D;
   const int lane = threadIdx.x & 63;
   const int lr = lane & 31;
@@ -244,10 +246,11 @@ __device__ __forceinline__ void key_loop(const float* __restrict__ qrow, bool ro
     float mx = sc[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-    const float mnew = fmaxf(m, pair_max(mx) * sl2);
+    // (SPLIT: scaled)
+    const float mnew = fmaxf(m, SPLIT ? pair_max(mx) * sl2 : pair_max(mx));
     // the outputs are rescaled only when some row's maximum rose
     if (__builtin_amdgcn_ballot_w64(!(mnew == m)) != 0) {
-      const float alpha = mnew == m ? 1.f : fast_exp2(m - mnew);
+      const float alpha = mnew == m ? 1.f : fast_exp2(SPLIT ? m - mnew : (m - mnew) * sl2);
       m = mnew;
       l *= alpha;
 #pragma unroll
@@ -262,7 +265,7 @@ __device__ __forceinline__ void key_loop(const float* __restrict__ qrow, bool ro
     float ls = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      sc[r] = fast_exp2(__builtin_fmaf(sc[r], sl2, -mm));
+      sc[r] = fast_exp2(SPLIT ? __builtin_fmaf(sc[r], sl2, -mm) : __builtin_fmaf(sc[r] - mm, sl2, low));
       ls += sc[r];
     }
     l += ls;
@@ -386,6 +389,19 @@ __device__ __forceinline__ void key_loop(const float* __restrict__ qrow, bool ro
       pv(buf, pp, sc);
     }
   }
+  if constexpr (!SPLIT) m = wide_max(m, sl2, low);
+}
+
+// Whether a first pass's state is out of range (a partial sum over eight waves
+// still fits below 2^120), or not finite.
+template <int DB>
+__device__ __forceinline__ bool state_out_of_range(const f32x16 (&o)[DB], float l) {
+  float hi = l;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) hi = __builtin_elementwise_maximum(hi, fabsf(o[db][r]));
+  return !(hi < 0x1p120f);
 }
 
 }  // namespace

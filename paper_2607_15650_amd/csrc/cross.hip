@@ -49,6 +49,7 @@ struct RowsCfg {
   static constexpr int RPL = 1024 / ROWB;          // rows per 1 KiB load
   static constexpr int LOADS = TILEB / 1024;       // 1 KiB loads of a tile
   static constexpr int LDS = 2 * NBUF * TILEB;
+  static_assert(NW * TILEB <= LDS, "a K and a V tile of 32 keys for every wave");
 };
 
 template <class C, int WPE, bool LIST>
@@ -147,8 +148,12 @@ __global__ __launch_bounds__(C::NT, WPE) void cross_kernel(const CrossArgs) {
     }
   }
 
-  // ---- the rows' state (two lanes' quarters of 16 dims make 32 bytes)
   a = args();
+  __syncthreads();                                   // the rings are done with
+  if (tiles > 0 && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o)) != 0)
+    wide_pass<D, LIST>(a, b, hk, key_begin, key_end, 32, smem + wave * C::TILEB, qf, o, m, l);
+
+  // ---- the rows' state (two lanes' quarters of 16 dims make 32 bytes)
   const float lt = pair_sum(l);
   const float inv = lt > 0.f ? 1.0f / lt : 0.f;
   const float lse = lt > 0.f ? (m + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
@@ -270,34 +275,46 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
     bad |= __shfl_xor(bad ? 1 : 0, d, 64) != 0;
   }
   const float mm = mx == -INFINITY ? 0.f : mx;
-  float tot = 0.f, w;
-  f32x4 acc = f32x4{};
+  // The weights' sums, in units of 2^low: 0, or 16 where the outputs of some
+  // ranges, near the type's largest, do not add up in float32 as they are (fewer
+  // than 2^16 ranges).
+  float tot, w, low = 0.f;
+  f32x4 acc;
   const float* src = a.part_out + r * D + lane * 4;
-  for (int p0 = 0; p0 < parts; p0 += TEAM) {
-    const float mine = p0 + lane < parts ? a.part_lse[(p0 + lane) * rows + r] : -INFINITY;
-    w = fast_exp2((mine - mm) * 1.4426950408889634f);
-    float sum = w;
+  for (;;) {
+    tot = 0.f;
+    acc = f32x4{};
+    for (int p0 = 0; p0 < parts; p0 += TEAM) {
+      const float mine = p0 + lane < parts ? a.part_lse[(p0 + lane) * rows + r] : -INFINITY;
+      w = fast_exp2((mine - mm) * 1.4426950408889634f - low);
+      float sum = w;
 #pragma unroll
-    for (int d = 1; d < TEAM; d <<= 1) sum += __shfl_xor(sum, d, 64);
-    tot += sum;
-    const int np = min(parts - p0, TEAM);
-    auto batch = [&](auto n, int q0) {
-      constexpr int N = decltype(n)::value;
-      f32x4 x[N];
+      for (int d = 1; d < TEAM; d <<= 1) sum += __shfl_xor(sum, d, 64);
+      tot += sum;
+      const int np = min(parts - p0, TEAM);
+      auto batch = [&](auto n, int q0) {
+        constexpr int N = decltype(n)::value;
+        f32x4 x[N];
 #pragma unroll
-      for (int q = 0; q < N; ++q) x[q] = *(const f32x4*)(src + (p0 + q0 + q) * rows * D);
+        for (int q = 0; q < N; ++q) x[q] = *(const f32x4*)(src + (p0 + q0 + q) * rows * D);
 #pragma unroll
-      for (int q = 0; q < N; ++q) {
-        const float wq = __shfl(w, first + q0 + q, 64);
+        for (int q = 0; q < N; ++q) {
+          const float wq = __shfl(w, first + q0 + q, 64);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wq, x[q][e], acc[e]);
-      }
-    };
-    int q0 = 0;
-    for (; q0 + 8 <= np; q0 += 8) batch(std::integral_constant<int, 8>{}, q0);
-    if (np & 4) batch(std::integral_constant<int, 4>{}, q0), q0 += 4;
-    if (np & 2) batch(std::integral_constant<int, 2>{}, q0), q0 += 2;
-    if (np & 1) batch(std::integral_constant<int, 1>{}, q0);
+          for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(wq, x[q][e], acc[e]);
+        }
+      };
+      int q0 = 0;
+      for (; q0 + 8 <= np; q0 += 8) batch(std::integral_constant<int, 8>{}, q0);
+      if (np & 4) batch(std::integral_constant<int, 4>{}, q0), q0 += 4;
+      if (np & 2) batch(std::integral_constant<int, 2>{}, q0), q0 += 2;
+      if (np & 1) batch(std::integral_constant<int, 1>{}, q0);
+    }
+    float hi = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hi = __builtin_elementwise_maximum(hi, fabsf(acc[e]));
+    if (low > 0.f || __builtin_amdgcn_ballot_w64(!(hi < INFINITY)) == 0) break;
+    low = 16.f;
   }
   if (at >= rows) return;
   const float inv = tot > 0.f ? 1.0f / tot : bad ? NAN : 0.f;
@@ -305,7 +322,7 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
   typedef T V __attribute__((ext_vector_type(4)));
   *(V*)((T*)a.out + ((b * a.q_len + tok) * a.H + h) * D + lane * 4) = __builtin_convertvector(acc * inv, V);
   if (lane == 0 && a.lse != nullptr)
-    a.lse[r] = tot > 0.f ? mx + __builtin_amdgcn_logf(tot) * kLn2 : bad ? NAN : -INFINITY;
+    a.lse[r] = tot > 0.f ? mx + (__builtin_amdgcn_logf(tot) + low) * kLn2 : bad ? NAN : -INFINITY;
 }
 
 template <class C, int WPE, bool LIST>

@@ -58,25 +58,25 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
 
   f32x16 o[C::DB];
   float m, l;
-  if (tid < 3) redo[tid] = 0;
+  if (tid < 4) redo[tid] = 0;
   uint64_t ask = 0;
   key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
   // what the planes cannot hold, as attn_f32_kernel finds it
-  float bad = l * 0.f, low = INFINITY;
+  const bool range = t0 < t1 && state_out_of_range(o, l);
+  float small_o = INFINITY;
 #pragma unroll
   for (int db = 0; db < C::DB; ++db)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      bad = __builtin_fmaf(o[db][r], 0.f, bad);
-      low = fminf(low, fabsf(o[db][r]));
-    }
+    for (int r = 0; r < 16; ++r) small_o = fminf(small_o, fabsf(o[db][r]));
   const float below = pair_sum(l) * 0x1p-100f;
-  const bool small = row_ok && low < below;
+  const bool small = row_ok && small_o < below;
   __syncthreads();
-  if ((__builtin_amdgcn_ballot_w64(!(bad == 0.f)) | ask) != 0 && lane == 0) redo[0] = 1;
+  if (ask != 0 && lane == 0) redo[0] = 1;
+  if (__builtin_amdgcn_ballot_w64(range) != 0 && lane == 0) redo[3] = 1;
   if (__builtin_amdgcn_ballot_w64(small) != 0 && lane == 0) redo[1] = 1;
   __syncthreads();
-  bool again = __builtin_amdgcn_readfirstlane(redo[0]) != 0;
+  const bool far = __builtin_amdgcn_readfirstlane(redo[3]) != 0;
+  bool again = far || __builtin_amdgcn_readfirstlane(redo[0]) != 0;
   if (!again && __builtin_amdgcn_readfirstlane(redo[1]) != 0) {
     constexpr int kBatch = 8;
     const int first = tb * C::BN;
@@ -99,7 +99,8 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
     again = __builtin_amdgcn_readfirstlane(redo[2]) != 0;
   }
   if (again) {
-    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
+    key_loop<C, false>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask,
+                       far ? wide_low(n) : 0.f);
     __syncthreads();
   }
 

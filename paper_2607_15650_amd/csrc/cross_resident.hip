@@ -117,40 +117,18 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
         dma_desc(desc, (uint32_t)r * (uint32_t)(stride * 2) + (uint32_t)unit * 16, dst);
       }
     }
-    auto load_queries = [&](int blk) {
+    auto load_queries = [&](int blk, int lane) {
       a = args();
       int tok, gi;
-      token_of(a, blk * 32, lr, &tok, &gi);
-      const __bf16* p = (const __bf16*)a->q + b * a->q_batch + tok * a->q_token + (int64_t)(hk * a->G + gi) * a->q_head + 8 * g;
+      token_of(a, blk * 32, lane & 31, &tok, &gi);
+      const __bf16* p = (const __bf16*)a->q + b * a->q_batch + tok * a->q_token + (int64_t)(hk * a->G + gi) * a->q_head +
+                        8 * (lane >> 5);
 #pragma unroll
       for (int s = 0; s < C::KS; ++s) qf[s] = *(const bf16x8*)(p + 16 * s);
     };
-    if (first + wave < last) load_queries(first + wave);
-    wait_loads();
-    __syncthreads();
-    for (int u = wave; u < tiles * 4; u += C::NW) fr.order_values(smem + (u / 4 * 2 + 1) * C::TILEB, u % 4);
-    __syncthreads();
-
-    for (int blk = first + wave; blk < last; blk += C::NW) {
-      f32x16 o[C::DB];
-      float m = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int db = 0; db < C::DB; ++db) o[db] = f32x16{};
-#pragma unroll 1
-      for (int i = 0; i < steps; ++i) {
-        const unsigned char* kt = smem + i / 2 * 2 * C::TILEB + i % 2 * 32 * C::ROWB;
-        f32x16 sc = fr.scores(kt, qf);
-        if (i + 1 == steps) {
-          load_queries(blk + C::NW < last ? blk + C::NW : blk);
-          if ((i + 1) * 32 > n) mask_keys(sc, n - i * 32, g);
-        }
-        bf16x8 pf[2];
-        softmax_step<C::DB>(sc, pf, o, m, l, sl2, i == 0);
-        fr.template values<true>(kt + C::TILEB, pf, o);
-      }
-      if (steps == 0) load_queries(blk + C::NW < last ? blk + C::NW : blk);
-
+    auto store_rows = [&](int blk, int lane, const f32x16 (&o)[C::DB], float m, float l) {
       a = args();
+      const int lr = lane & 31, g = lane >> 5;
       // ---- the rows' state: two lanes' quarters of 16 dims make rows of 32 bytes
       const float lt = pair_sum(l);
       const float inv = lt > 0.f ? 1.0f / lt : 0.f;
@@ -168,6 +146,58 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
 #pragma unroll
           for (int half = 0; half < 2; ++half) *(bf16x8*)(dst + 32 * db + 16 * half) = row_units(o[db], half, inv);
       }
+    };
+    if (first + wave < last) load_queries(first + wave, lane);
+    wait_loads();
+    __syncthreads();
+    for (int u = wave; u < tiles * 4; u += C::NW) fr.order_values(smem + (u / 4 * 2 + 1) * C::TILEB, u % 4);
+    __syncthreads();
+
+    uint64_t again = 0;
+    for (int blk = first + wave, turn = 0; blk < last; blk += C::NW, ++turn) {
+      f32x16 o[C::DB];
+      float m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db) o[db] = f32x16{};
+#pragma unroll 1
+      for (int i = 0; i < steps; ++i) {
+        const unsigned char* kt = smem + i / 2 * 2 * C::TILEB + i % 2 * 32 * C::ROWB;
+        f32x16 sc = fr.scores(kt, qf);
+        if (i + 1 == steps) {
+          load_queries(blk + C::NW < last ? blk + C::NW : blk, lane);
+          if ((i + 1) * 32 > n) mask_keys(sc, n - i * 32, g);
+        }
+        bf16x8 pf[2];
+        softmax_step<C::DB>(sc, pf, o, m, l, sl2, i == 0);
+        fr.template values<true>(kt + C::TILEB, pf, o);
+      }
+      if (steps == 0) load_queries(blk + C::NW < last ? blk + C::NW : blk, lane);
+      // (a bit for every 64th of the wave's blocks)
+      if (steps > 0 && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o)) != 0) again |= 1ull << (turn & 63);
+      store_rows(blk, lane, o, m, l);
+    }
+    if (again == 0) continue;
+    // ---- the blocks with rows out of range once more, over the rows as stored
+    wait_loads();
+    for (int blk = first + wave, turn = 0; blk < last; blk += C::NW, ++turn) {
+      if ((again >> (turn & 63) & 1) == 0) continue;
+      const FragReader<D> wr(lane_id());
+      load_queries(blk, wr.lane);
+      f32x16 o[C::DB];
+      const float low = wide_low(n);
+      float mx = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db) o[db] = f32x16{};
+#pragma unroll 1
+      for (int i = 0; i < steps; ++i) {
+        const unsigned char* kt = smem + i / 2 * 2 * C::TILEB + i % 2 * 32 * C::ROWB;
+        f32x16 sc = wr.scores(kt, qf);
+        if ((i + 1) * 32 > n) mask_keys(sc, n - i * 32, wr.lane >> 5);
+        bf16x8 pf[2];
+        wide_step<C::DB>(sc, pf, o, mx, l, sl2, low);
+        wr.template values<true>(kt + C::TILEB, pf, o);
+      }
+      store_rows(blk, wr.lane, o, wide_max(mx, sl2, low), l);
     }
   }
 }

@@ -38,7 +38,7 @@ struct TaskCfg {
   static constexpr int EXTRA = RING + 1024;
   static constexpr int LDS = EXTRA + STAGE;
   static constexpr int NQ = QB * KS / 4;            // registers of query rows, by 16
-  static_assert(STAGE == TILEB, "a wave's output rows take one ring slot");
+  static_assert(STAGE == TILEB, "a wave's output rows take one ring slot, as a K and a V tile of 32 keys do");
   // Where a wave's output rows are staged: ring slots that the next task's
   // first tiles (K 0 ... 2, V 0 and 1) do not go to, then past the ring.
   static constexpr __device__ int stage(int wave) {
@@ -50,12 +50,6 @@ struct TaskCfg {
 // loop's (attn_bf16.hip).
 constexpr float kRowSumBound = 1099511627776.0f;   // 2^40
 
-// This lane of the wave, counted anew.
-__device__ __forceinline__ int lane_id() {
-  int x;
-  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
-  return x;
-}
 // x / d for wave-uniform 0 <= x < 2^31, with 2^32 / d rounded down (d = 1:
 // 2^32 - 1): the product's high half is the quotient or one less.
 __device__ __forceinline__ int divide(int x, int d, uint32_t inverse) {
@@ -63,6 +57,59 @@ __device__ __forceinline__ int divide(int x, int d, uint32_t inverse) {
   return q + (x - q * d >= d ? 1 : 0);
 }
 inline uint32_t inverse_of(int d) { return d == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / (uint32_t)d); }
+
+// The query blocks of `which` (a bit each) of a wave's rows, formed by wide_pass
+// and stored.
+template <int D>
+__device__ __forceinline__ void form_again(Args a, int b, int hk, int part, int row0, int wave, uint32_t which,
+                                           unsigned char* own) {
+  using C = TaskCfg<D>;
+  const int n = __builtin_amdgcn_readfirstlane(live_keys(a, b));
+  const int per = ((n + C::BN - 1) / C::BN + a->split - 1) / a->split * C::BN;
+  const int first = min(part * per, n), end = min(first + per, n);
+  const int lane = lane_id();
+  const int lr = lane & 31, g = lane >> 5;
+  wait_loads();                                      // (the rows as stored first)
+#pragma unroll 1
+  for (int qb = 0; qb < C::QB; ++qb) {
+    if ((which >> qb & 1) == 0) continue;
+    const int r = (wave * C::QB + qb) * 32 + lr;
+    int tok, gi;
+    token_of(a, row0, r, &tok, &gi);
+    const __bf16* p = (const __bf16*)a->q + b * a->q_batch + tok * a->q_token + (int64_t)(hk * a->G + gi) * a->q_head + 8 * g;
+    bf16x8 qf[C::KS];
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) qf[s] = *(const bf16x8*)(p + 16 * s);
+    f32x16 o[C::DB];
+    float m, l;
+    wide_pass<D, false>(a, b, hk, first, end, 32, own, qf, o, m, l);
+    const float lt = pair_sum(l), inv = lt > 0.f ? 1.0f / lt : 0.f;
+    const float lse = lt > 0.f ? (m + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
+    if (row0 + r >= a->rows) continue;
+    const int h = hk * a->G + gi;
+    const int64_t at = ((int64_t)b * a->H + h) * a->q_len + tok;
+    if (a->split > 1) {
+      const int64_t ap = (int64_t)part * a->B * a->H * a->q_len + at;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = o[db][4 * r4 + e] * inv;
+          *(f32x4*)(a->part_out + ap * D + 4 * g + db * 32 + 8 * r4) = x;
+        }
+      if (g == 0) a->part_lse[ap] = lse;
+    } else {
+      __bf16* dst = (__bf16*)a->out + (((int64_t)b * a->q_len + tok) * a->H + h) * D + 8 * g;
+#pragma unroll
+      for (int db = 0; db < C::DB; ++db)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) *(bf16x8*)(dst + 32 * db + 16 * half) = row_units(o[db], half, inv);
+      if (g == 0 && a->lse != nullptr) a->lse[at] = lse;
+    }
+  }
+}
 
 template <int D_>
 __global__ __launch_bounds__(256, 1) void cross_task_kernel(const CrossArgs) {
@@ -304,6 +351,11 @@ asm volatile(BODY                                                               
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[qb][db] = f32x16{};
     }
+    // the query blocks whose state left the range
+    uint32_t again = 0;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb)
+      if (keys && __builtin_amdgcn_ballot_w64(out_of_range<DB>(o[qb])) != 0) again |= 1u << qb;
 
     if (a->split > 1) {
       // ---- the partial state of a key range, as it lies in the registers
@@ -331,73 +383,73 @@ asm volatile(BODY                                                               
             a->part_lse[at] = lt > 0.f ? (m[qb] + __builtin_amdgcn_logf(lt)) * kLn2 : lt == 0.f ? -INFINITY : lt;
         }
       }
-      if (!more) break;
-      at += step;
-      t = next;
-      continue;
-    }
-    // ---- the rows' state: through LDS (16-byte units swizzled by row, the
-    // halves of a unit by row / 16), then stored whole
-    unsigned char* stage = smem + C::stage(wave);
-    auto swz_out = [](int row) { return row & (C::UNITS - 1); };
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const float lt = keys ? pair_sum(l[qb]) : 0.f;
-      const float inv = lt > 0.f ? 1.0f / lt : 0.f;
-      unsigned char* srow = stage + (qb * 32 + lr) * C::ROWB;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          f32x4 x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = o[qb][db][4 * r4 + e] * inv;
-          const int unit = (4 * db + r4) ^ swz_out(qb * 32 + lr);
-          *(bf16x4*)(srow + unit * 16 + 8 * (g ^ ((lr >> 4) & 1))) = __builtin_convertvector(x, bf16x4);
-        }
-      l[qb] = lt;
-    }
-    const int out_row = lane / C::UNITS, out_unit = lane % C::UNITS;
-    bf16x8 x[QB * 32 / C::RPL];
-#pragma unroll
-    for (int i = 0; i < QB * 32 / C::RPL; ++i) {
-      const int row = i * C::RPL + out_row;
-      x[i] = *(const bf16x8*)(stage + row * C::ROWB + ((out_unit ^ swz_out(row)) * 16));
-      if ((row >> 4) & 1) x[i] = __builtin_shufflevector(x[i], x[i], 4, 5, 6, 7, 0, 1, 2, 3);
-    }
-    landed();
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      const int r = (wave * QB + qb) * 32 + lr;
-      if (g == 0 && a->lse != nullptr && t.row0 + r < a->rows) {
-        int tok, gi;
-        token_of(a, t.row0, r, &tok, &gi);
-        a->lse[((int64_t)t.b * a->H + t.hk * a->G + gi) * a->q_len + tok] =
-            l[qb] > 0.f ? (m[qb] + __builtin_amdgcn_logf(l[qb])) * kLn2 : l[qb] == 0.f ? -INFINITY : l[qb];
-      }
-    }
-    const int64_t out_row_elems = (int64_t)a->H * D;
-    __bf16* out = (__bf16*)a->out + ((int64_t)t.b * a->q_len * a->H + t.hk * a->G) * D + out_unit * 8;
-    if (a->G == 1) {
-      // rows at a fixed distance
-      const int r0 = t.row0 + wave * QB * 32 + out_row;
-      __bf16* p = out + r0 * out_row_elems;
-#pragma unroll
-      for (int i = 0; i < QB * 32 / C::RPL; ++i) {
-        if (r0 + i * C::RPL < a->rows) __builtin_nontemporal_store(x[i], (bf16x8*)p);
-        p += C::RPL * out_row_elems;
-      }
     } else {
+      // ---- the rows' state: through LDS (16-byte units swizzled by row, the
+      // halves of a unit by row / 16), then stored whole
+      unsigned char* stage = smem + C::stage(wave);
+      auto swz_out = [](int row) { return row & (C::UNITS - 1); };
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const float lt = keys ? pair_sum(l[qb]) : 0.f;
+        const float inv = lt > 0.f ? 1.0f / lt : 0.f;
+        unsigned char* srow = stage + (qb * 32 + lr) * C::ROWB;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = o[qb][db][4 * r4 + e] * inv;
+            const int unit = (4 * db + r4) ^ swz_out(qb * 32 + lr);
+            *(bf16x4*)(srow + unit * 16 + 8 * (g ^ ((lr >> 4) & 1))) = __builtin_convertvector(x, bf16x4);
+          }
+        l[qb] = lt;
+      }
+      const int out_row = lane / C::UNITS, out_unit = lane % C::UNITS;
+      bf16x8 x[QB * 32 / C::RPL];
 #pragma unroll
       for (int i = 0; i < QB * 32 / C::RPL; ++i) {
-        const int r = wave * QB * 32 + i * C::RPL + out_row;
-        if (t.row0 + r < a->rows) {
+        const int row = i * C::RPL + out_row;
+        x[i] = *(const bf16x8*)(stage + row * C::ROWB + ((out_unit ^ swz_out(row)) * 16));
+        if ((row >> 4) & 1) x[i] = __builtin_shufflevector(x[i], x[i], 4, 5, 6, 7, 0, 1, 2, 3);
+      }
+      landed();
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        const int r = (wave * QB + qb) * 32 + lr;
+        if (g == 0 && a->lse != nullptr && t.row0 + r < a->rows) {
           int tok, gi;
           token_of(a, t.row0, r, &tok, &gi);
-          __builtin_nontemporal_store(x[i], (bf16x8*)(out + tok * out_row_elems + gi * D));
+          a->lse[((int64_t)t.b * a->H + t.hk * a->G + gi) * a->q_len + tok] =
+              l[qb] > 0.f ? (m[qb] + __builtin_amdgcn_logf(l[qb])) * kLn2 : l[qb] == 0.f ? -INFINITY : l[qb];
+        }
+      }
+      const int64_t out_row_elems = (int64_t)a->H * D;
+      __bf16* out = (__bf16*)a->out + ((int64_t)t.b * a->q_len * a->H + t.hk * a->G) * D + out_unit * 8;
+      if (a->G == 1) {
+        // rows at a fixed distance
+        const int r0 = t.row0 + wave * QB * 32 + out_row;
+        __bf16* p = out + r0 * out_row_elems;
+#pragma unroll
+        for (int i = 0; i < QB * 32 / C::RPL; ++i) {
+          if (r0 + i * C::RPL < a->rows) __builtin_nontemporal_store(x[i], (bf16x8*)p);
+          p += C::RPL * out_row_elems;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < QB * 32 / C::RPL; ++i) {
+          const int r = wave * QB * 32 + i * C::RPL + out_row;
+          if (t.row0 + r < a->rows) {
+            int tok, gi;
+            token_of(a, t.row0, r, &tok, &gi);
+            __builtin_nontemporal_store(x[i], (bf16x8*)(out + tok * out_row_elems + gi * D));
+          }
         }
       }
     }
+    // ---- those that left the range: once more, by this wave alone, over the
+    // rows as stored, in the LDS they were staged in
+    if (again != 0) form_again<D>(a, t.b, t.hk, t.part, t.row0, wave, again, smem + C::stage(wave));
     if (!more) break;
     at += step;
     t = next;

@@ -26,6 +26,14 @@ __device__ __forceinline__ int live_keys(Args a, int b) {
   return a->lens == nullptr ? a->kv_len : min(max(a->lens[b], 0), a->kv_len);
 }
 
+// This lane of the wave, counted anew: what a rare path derives from it is not
+// computed, and kept, in front of the loops around that path.
+__device__ __forceinline__ int lane_id() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+  return x;
+}
+
 // Token and head (of the G that share a key/value head) of row row0 + r; rows
 // past the end give the last one's.  row0 is wave-uniform.
 __device__ __forceinline__ void token_of(Args a, int row0, int r, int* tok, int* gi) {
@@ -141,7 +149,9 @@ __device__ __forceinline__ void mask_keys(f32x16& sc, int left, int g) {
 // Scores of 32 keys -> probabilities against the running maximum m, row sum l
 // (this lane's keys).  m is the first step's maximum, and raised only where a
 // lane's sum over a step then passes 2^40 or is not a number: below that
-// float32 holds the sums, and the result does not depend on which m was used.
+// float32 holds the row sums, and the result does not depend on which m was
+// used.  It holds the outputs too while the values are below 2^80 or so;
+// out_of_range finds the rows where it does not.
 template <int DB>
 __device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], f32x16 (&o)[DB], float& m, float& l,
                                              float sl2, bool first) {
@@ -181,6 +191,101 @@ __device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], 
     probs();
   }
   l += sum;
+}
+
+// What the steps above cannot hold: a row whose probabilities, up to 2^40 of
+// them against a lagging maximum, or whose number took an output to 2^120 or
+// more (four partial ones below that add up inside float32).  NaN and infinities
+// are among them.  Such rows are formed again, by wide_pass.  (Beside the
+// exponentials: cross_video 119.4 -> 120.1 us, 9,450 rows x 40 heads against 256
+// keys 74.0 -> 75.2.)
+template <int DB>
+__device__ __forceinline__ bool out_of_range(const f32x16 (&o)[DB]) {
+  float hi = 0.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) hi = __builtin_elementwise_maximum(hi, fabsf(o[db][r]));
+  return !(hi < 0x1p120f);
+}
+
+// Scores of 32 keys -> probabilities 2^low exp2(scale (s - mx)) against the
+// maximum mx of the scores so far as they are: the largest is 2^low exactly
+// (attn_tile.h has low, by which sums over all keys stay below the values they
+// weigh).
+template <int DB>
+__device__ __forceinline__ void wide_step(const f32x16& sc, bf16x8 (&pf)[2], f32x16 (&o)[DB], float& mx, float& l,
+                                          float sl2, float low) {
+  float top = sc[0];
+#pragma unroll
+  for (int r = 1; r < 16; ++r) top = fmaxf(top, sc[r]);
+  const float mnew = fmaxf(mx, pair_max(top));
+  const float at = mnew == -INFINITY ? 0.f : mnew;
+  const float alpha = mx == -INFINITY ? 0.f : fast_exp2((mx - mnew) * sl2);
+  mx = mnew;
+  l *= alpha;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] *= alpha;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    f32x8 x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = fast_exp2(__builtin_fmaf(sc[8 * h + e] - at, sl2, low));
+      l += x[e];
+    }
+    pf[h] = __builtin_convertvector(x, bf16x8);
+  }
+}
+// The state of 32 rows over keys [key_begin, key_end) in steps of 32 that lie
+// `stride` apart, by one wave: tiles of 32 keys of K and of V in LDS of its own,
+// loaded as they are needed (rows out of range are rare: simple, not fast).
+template <int D, bool LIST>
+__device__ __forceinline__ void wide_pass(Args a, int b, int hk, int key_begin, int key_end, int stride,
+                                          unsigned char* own, const bf16x8 (&qf)[D / 16], f32x16 (&o)[D / 32], float& m,
+                                          float& l) {
+  constexpr int ROWB = D * 2, UNITS = D / 8, RPL = 1024 / ROWB;
+  const __bf16* kg = (const __bf16*)a->k + b * a->k_batch + hk * a->k_head;
+  const __bf16* vg = (const __bf16*)a->v + b * a->v_batch + hk * a->v_head;
+  const int32_t* list = LIST ? a->list + (int64_t)b * a->kv_len : nullptr;
+  const float sl2 = a->scale_log2, low = wide_low(key_end - key_begin);
+  const int lane = lane_id();
+  const FragReader<D> fr(lane);
+  float mx = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) o[db] = f32x16{};
+#pragma unroll 1
+  for (int64_t key = key_begin; key < key_end; key += stride) {
+    const int left = (int)min(key_end - key, (int64_t)32);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the last step's reads are back
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+      for (int j = 0; j < 32 / RPL; ++j) {
+        const int r = j * RPL + lane / UNITS;
+        const int unit = lane % UNITS ^ (which ? swz_v<D>(r) : swz_k<D>(r));
+        // (rows past the end read the last one: its scores are masked, and its
+        // values replaced by zeros)
+        const int64_t at = key + min(r, left - 1);
+        const __bf16* p = (which ? vg : kg) + (LIST ? (int64_t)list[at] : at) * (which ? a->v_token : a->k_token);
+        dma_addr(p + unit * 8, lds_addr(own) + (uint32_t)(which * 32 * ROWB + j * 1024));
+      }
+    wait_loads();
+    if (left < 32) {
+      uint32_t zero = 0;
+      asm volatile("" : "+v"(zero));                       // (not kept in registers around the loops outside)
+      for (int i = lane; i < (32 - left) * UNITS; i += 64)
+        *(u32x4*)(own + (32 + left) * ROWB + i * 16) = u32x4{zero, zero, zero, zero};
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    f32x16 sc = fr.scores(own, qf);
+    if (left < 32) mask_keys(sc, left, lane >> 5);
+    bf16x8 pf[2];
+    wide_step<D / 32>(sc, pf, o, mx, l, sl2, low);
+    fr.template values<false>(own + 32 * ROWB, pf, o);
+  }
+  m = wide_max(mx, sl2, low);
 }
 
 // Unit `half` of a lane's row in a 32-dim block of the accumulators, times
