@@ -21,10 +21,11 @@
 //   have an accumulator of their own.
 //   What the planes cannot hold goes through the float32 MFMA: a workgroup
 //   runs its task again with it
-//    - where some row's sum or output ends up not finite, or beyond 2^120
-//      (state_out_of_range).  A value that is not finite, or rounds to infinity
-//      in bf16, gives NaN in the planes and in every row it enters; the float32
-//      MFMA treats infinities as float32 arithmetic does;
+//    - where some row's sum or output ends up not finite, or beyond 2^120, or
+//      its maximum at 2^24 or more (state_out_of_range).  A value that is not
+//      finite, or rounds to infinity in bf16, gives NaN in the planes and in
+//      every row it enters; the float32 MFMA treats infinities as float32
+//      arithmetic does;
 //    - where nonzero values below 2^-110 matter.  Their third plane falls
 //      under bf16's smallest subnormal (2^-133), so such a value is off by up
 //      to 2^-134.  Its queries are looked at as they are split: one of these
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(C::NT, C::WPE) void attn_f32_kernel(const AttnArgs 
   if (tid < 4) redo[tid] = 0;
   uint64_t ask = 0;
   key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
-  const bool range = t0 < t1 && state_out_of_range(o, l);
+  const bool range = t0 < t1 && state_out_of_range(o, m, l);
   float small_o = INFINITY;
 #pragma unroll
   for (int db = 0; db < C::DB; ++db)

@@ -393,10 +393,11 @@ __device__ __forceinline__ void key_loop(const float* __restrict__ qrow, bool ro
 }
 
 // Whether a first pass's state is out of range (a partial sum over eight waves
-// still fits below 2^120), or not finite.
+// still fits below 2^120): not finite, or against a maximum whose rounding after
+// the scaling the exponents' fused products do not share.
 template <int DB>
-__device__ __forceinline__ bool state_out_of_range(const f32x16 (&o)[DB], float l) {
-  float hi = l;
+__device__ __forceinline__ bool state_out_of_range(const f32x16 (&o)[DB], float m, float l) {
+  float hi = __builtin_elementwise_maximum(fabsf(m) * 0x1p96f, l);
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll

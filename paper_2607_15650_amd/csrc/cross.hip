@@ -150,7 +150,7 @@ __global__ __launch_bounds__(C::NT, WPE) void cross_kernel(const CrossArgs) {
 
   a = args();
   __syncthreads();                                   // the rings are done with
-  if (tiles > 0 && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o)) != 0)
+  if (tiles > 0 && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o, m)) != 0)
     wide_pass<D, LIST>(a, b, hk, key_begin, key_end, 32, smem + wave * C::TILEB, qf, o, m, l);
 
   // ---- the rows' state (two lanes' quarters of 16 dims make 32 bytes)

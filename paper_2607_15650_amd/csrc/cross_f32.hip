@@ -62,7 +62,7 @@ __global__ __launch_bounds__(C::NT, C::WPE) void cross_f32_kernel(const CrossArg
   uint64_t ask = 0;
   key_loop<C, true>(qrow, row_ok, kr, vr, kv_len, t0, t1, a.scale_log2, kb, gt, o, m, l, ask);
   // what the planes cannot hold, as attn_f32_kernel finds it
-  const bool range = t0 < t1 && state_out_of_range(o, l);
+  const bool range = t0 < t1 && state_out_of_range(o, m, l);
   float small_o = INFINITY;
 #pragma unroll
   for (int db = 0; db < C::DB; ++db)

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(C::NT, 2) void cross_few_kernel(const CrossArgs) {
   }
 
   a = args();
-  if (wave < tiles && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o)) != 0)
+  if (wave < tiles && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o, m)) != 0)
     wide_pass<D, LIST>(a, b, hk, key_begin + wave * BN, key_end, C::NW * BN, mine, qf, o, m, l);
 
   // ---- the four partial states: O rows of 16-byte units, swizzled by row

@@ -173,7 +173,7 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
       }
       if (steps == 0) load_queries(blk + C::NW < last ? blk + C::NW : blk, lane);
       // (a bit for every 64th of the wave's blocks)
-      if (steps > 0 && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o)) != 0) again |= 1ull << (turn & 63);
+      if (steps > 0 && __builtin_amdgcn_ballot_w64(out_of_range<C::DB>(o, m)) != 0) again |= 1ull << (turn & 63);
       store_rows(blk, lane, o, m, l);
     }
     if (again == 0) continue;

@@ -355,7 +355,7 @@ asm volatile(BODY                                                               
     uint32_t again = 0;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb)
-      if (keys && __builtin_amdgcn_ballot_w64(out_of_range<DB>(o[qb])) != 0) again |= 1u << qb;
+      if (keys && __builtin_amdgcn_ballot_w64(out_of_range<DB>(o[qb], m[qb])) != 0) again |= 1u << qb;
 
     if (a->split > 1) {
       // ---- the partial state of a key range, as it lies in the registers

@@ -195,13 +195,16 @@ __device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], 
 
 // What the steps above cannot hold: a row whose probabilities, up to 2^40 of
 // them against a lagging maximum, or whose number took an output to 2^120 or
-// more (four partial ones below that add up inside float32).  NaN and infinities
-// are among them.  Such rows are formed again, by wide_pass.  (Beside the
-// exponentials: cross_video 119.4 -> 120.1 us, 9,450 rows x 40 heads against 256
-// keys 74.0 -> 75.2.)
+// more (four partial ones below that add up inside float32), or whose maximum is
+// 2^24 or more.  There the rounding of m, which the exponents' fused products do
+// not share, moves every probability by a factor that passes 2^(1/2), and from
+// 2^31 on can leave float32's range: 0 for all, or infinity.  NaN and infinities
+// are among them, and a row whose every score was -inf.  Such rows are formed
+// again, by wide_pass.  (Beside the exponentials: cross_video 119.4 -> 120.1 us,
+// 9,450 rows x 40 heads against 256 keys 74.0 -> 75.2.)
 template <int DB>
-__device__ __forceinline__ bool out_of_range(const f32x16 (&o)[DB]) {
-  float hi = 0.f;
+__device__ __forceinline__ bool out_of_range(const f32x16 (&o)[DB], float m) {
+  float hi = fabsf(m) * 0x1p96f;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll

@@ -73,3 +73,47 @@ def test_values_near_the_largest(gpu_lib, dtype, Lq, S, H, D, kind):
     v = v.to(dtype)
     live, kw = masked(kind, S)
     check(CrossAttention(D ** -0.5)(q, k, v, **kw), q, k, v, D ** -0.5, live)
+
+
+def gap(q, k, scale, live):
+    """Of every row: how far the largest score lies above the next, and what
+    float32 may be off by in them: 2^-24 of sum |q k| scale for each of D products
+    and sums, at most."""
+    top, off = [], []
+    for h in range(q.shape[2]):
+        a, b = q[0, :, h].double(), k[0, live[0], h].double().T.contiguous()
+        t = (a @ b * scale).topk(2, dim=1).values
+        top.append((t[:, 0] - t[:, 1]).cpu())
+        off.append((a.abs() @ b.abs()).max(dim=1).values.cpu() * scale * 2.0 ** -24 * q.shape[3])
+    return torch.stack(top), torch.stack(off)
+
+
+@pytest.mark.parametrize("kind", ["all", "mask"])
+@pytest.mark.parametrize("dtype,Lq,S,H,D", FORMS)
+def test_large_scores(gpu_lib, dtype, Lq, S, H, D, kind):
+    """Scores of 1e8 ... 1e30, in rows beside ordinary ones: the largest takes all."""
+    from paper_2607_15650_amd.cross import CrossAttention
+    g = torch.Generator(device="cuda")
+    g.manual_seed(S + 1)
+    k = torch.randn(1, S, H, D, generator=g, device="cuda") * 1e4
+    q = torch.randn(1, Lq, H, D, generator=g, device="cuda")
+    power = torch.randint(4, 27, (1, Lq, H, 1), generator=g, device="cuda").float()
+    power[:, ::5] = -4.0
+    q, k = (q * 10.0 ** power).to(dtype), k.to(dtype)
+    v = torch.randn(1, S, H, D, generator=g, device="cuda").to(dtype)
+    live, kw = masked(kind, S)
+    scale = 1.1 * D ** -0.5
+    out, lse = (x.double().cpu() for x in CrossAttention(scale)(q, k, v, **kw))
+    want, el, apart = reference(q, k, v, scale, live, "cuda")
+    assert torch.isfinite(lse).all() and torch.isfinite(out).all()
+    # scores off by `off` each, and the float32 scale and its product with log2(e)
+    d, off = gap(q, k, scale, live)
+    assert bool(((lse - el).abs()[0] <= 1e-5 * (1 + el.abs()[0]) + off + 2.0 ** -21 * el.abs()[0]).all())
+    ordinary = (power[0, :, :, 0] < 0).cpu()
+    over = ((out - want).abs() - tolerance(dtype, want, apart, float(v.double().abs().max())))[0].amax(-1)
+    assert float(over[ordinary].max()) <= 0
+    # the largest stays it by 30 at least, and takes all: its value, one product and one rounding
+    clear = (d > 2 * off + 30).T & ~ordinary
+    assert int(clear.sum()) * 2 >= int((~ordinary).sum())
+    one = (out - want).abs()[0] - 2.0 ** (-8 if dtype == BF16 else -22) * want.abs()[0] - 2.0 ** -40
+    assert float(one.amax(-1)[clear].max()) <= 0 if bool(clear.any()) else True
