@@ -10,13 +10,17 @@ import torch
 
 from . import api
 
+# elements between tokens: any number for queries, below 2^24 for keys and values
+_FAR, _KEYS_APART = 1 << 62, (1 << 24) - 1
 
-def _rows(x: torch.Tensor) -> torch.Tensor:
+
+def _rows(x: torch.Tensor, most: int) -> torch.Tensor:
     """``x`` itself where the kernels read it in place (rows of contiguous
-    elements, addresses and strides of 16 bytes), or a dense copy."""
+    elements, addresses and strides of 16 bytes, tokens at most ``most``
+    elements apart), or a dense copy."""
     e = x.element_size()
     s0, s1, s2, s3 = x.stride()
-    if s3 == 1 and not (x.data_ptr() | s0 * e | s1 * e | s2 * e) & 15:
+    if s3 == 1 and s1 <= most and not (x.data_ptr() | s0 * e | s1 * e | s2 * e) & 15:
         return x
     return x.clone(memory_format=torch.contiguous_format)
 
@@ -55,7 +59,7 @@ class CrossAttention:
         """(OUT [B, q_len, H, D], LSE [B, H, q_len]) of q [B, q_len, H, D] over the
         live keys of k, v [B, kv_len, Hk, D].  Tensors that the kernels cannot
         read in place are copied first."""
-        q, k, v = _rows(q), _rows(k), _rows(v)
+        q, k, v = _rows(q, _FAR), _rows(k, _KEYS_APART), _rows(v, _KEYS_APART)
         B, q_len, H, D = q.shape
         out = q.new_empty((B, q_len, H, D))
         lse = q.new_empty((B, H, q_len), dtype=torch.float32)

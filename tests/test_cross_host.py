@@ -1,0 +1,44 @@
+"""Host side of the cross attention's and the rotary inputs' classes, without a
+GPU: what they hand over and copy, and the buffers they keep (the calls are
+recorded, nothing is computed)."""
+import pytest
+import torch
+
+from paper_2607_15650_amd import api
+from paper_2607_15650_amd.cross import CrossAttention
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Arguments of every cross_attn call; each wants the workspace that `need` says."""
+    log, need = [], {"bytes": 0}
+    monkeypatch.setattr(api, "cross_attn", lambda *a: log.append(a))
+    monkeypatch.setattr(api, "cross_attn_workspace_bytes", lambda *a: need["bytes"])
+    return log, need
+
+
+def test_rows_that_cannot_be_read_in_place_are_copied(calls):
+    log, _ = calls
+    buf = torch.arange(1 << 25, dtype=torch.int32).to(BF16)
+
+    def rows(stride, heads=64, at=0):
+        return torch.as_strided(buf, (1, 2, 2, 64), (0, stride, heads, 1), at)
+
+    def handed(**kw):
+        x = {**dict(q=rows(256), k=rows(256), v=rows(256)), **kw}
+        CrossAttention(0.125)(**x)
+        got = dict(zip("qkv", log[-1][:3]))
+        assert all(torch.equal(got[n], x[n]) for n in "qkv")
+        return {n for n in "qkv" if got[n].data_ptr() == x[n].data_ptr() and got[n].stride() == x[n].stride()}
+
+    far = 1 << 24
+    assert handed() == {"q", "k", "v"}
+    # keys and values below 2^24 elements apart stay, queries at any distance
+    assert handed(q=rows(far), k=rows(far - 8), v=rows(far - 8)) == {"q", "k", "v"}
+    assert handed(k=rows(far)) == {"q", "v"}
+    assert handed(v=rows(far + 8)) == {"q", "k"}
+    for bad in (rows(257), rows(256, heads=68), rows(256, at=1)):
+        for n in "qkv":
+            assert handed(**{n: bad}) == set("qkv") - {n}
