@@ -4,7 +4,7 @@ this module owns the workspace and the outputs.
 """
 from __future__ import annotations
 
-from typing import Optional, Tuple
+from typing import Dict, Optional, Tuple
 
 import torch
 
@@ -27,18 +27,19 @@ def _rows(x: torch.Tensor, most: int) -> torch.Tensor:
 
 class CrossAttention:
     """Attention of query blocks to encoder states, with the workspace kept
-    across calls (it only grows).  The calls of one instance share it: order
-    them on one stream, or across streams by events.  A workspace that became
-    too small stays allocated, for graphs captured with it."""
+    across calls (one of each device, which only grows).  The calls of one
+    instance share it: order them on one stream, or across streams by events.  A
+    workspace that became too small stays allocated, for graphs captured with
+    it."""
 
     def __init__(self, scale: float):
         self.scale = float(scale)
-        self._ws: Optional[torch.Tensor] = None
+        self._ws: Dict[torch.device, torch.Tensor] = {}
         self._kept = []
         self._bytes = {}
 
     def _workspace(self, q, k, masked: bool) -> Optional[torch.Tensor]:
-        key = (q.dtype, q.shape, k.shape, masked)
+        key = (q.device, q.dtype, q.shape, k.shape, masked)
         n = self._bytes.get(key)
         if n is None:
             if len(self._bytes) >= 4096:
@@ -47,12 +48,13 @@ class CrossAttention:
                 q.dtype, q.shape[0], q.shape[2], k.shape[2], q.shape[3], q.shape[1], k.shape[1], masked)
         if n == 0:
             return None
-        if self._ws is None or self._ws.numel() < n or self._ws.device != q.device:
-            if self._ws is not None:
-                self._kept.append(self._ws)
-                n = max(n, 2 * self._ws.numel())     # what is kept stays below what is in use
-            self._ws = torch.empty(n, dtype=torch.uint8, device=q.device)
-        return self._ws
+        ws = self._ws.get(q.device)
+        if ws is None or ws.numel() < n:
+            if ws is not None:
+                self._kept.append(ws)
+                n = max(n, 2 * ws.numel())           # what is kept stays below what is in use
+            ws = self._ws[q.device] = torch.empty(n, dtype=torch.uint8, device=q.device)
+        return ws
 
     def __call__(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv_lens: Optional[torch.Tensor] = None,
                  key_mask: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -42,3 +42,23 @@ def test_rows_that_cannot_be_read_in_place_are_copied(calls):
     for bad in (rows(257), rows(256, heads=68), rows(256, at=1)):
         for n in "qkv":
             assert handed(**{n: bad}) == set("qkv") - {n}
+
+
+def test_each_device_has_its_workspace(calls):
+    """Calls on two devices in turn keep one buffer each, however many they are; a
+    larger call keeps the smaller one's for graphs that hold it."""
+    log, need = calls
+    need["bytes"] = 1000
+    op = CrossAttention(0.125)
+    x = torch.zeros(1, 2, 2, 64, dtype=BF16)
+    y = x.to("meta")
+    for _ in range(4):
+        for t in (x, y):
+            op(t, t, t)
+    used = [a[-1] for a in log]
+    assert all(w.device == a[0].device and w.numel() == 1000 for w, a in zip(used, log))
+    assert all(w is used[i % 2] for i, w in enumerate(used)) and not op._kept
+    need["bytes"] = 1500
+    z = torch.zeros(1, 3, 2, 64, dtype=BF16)
+    op(z, x, x)
+    assert log[-1][-1].numel() >= 1500 and len(op._kept) == 1 and op._kept[0] is used[0]
