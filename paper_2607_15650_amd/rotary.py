@@ -128,17 +128,20 @@ class RotatedInputs:
         self.rotary = rotary
         self.offsets = [int(o) for o in offsets]
         self.most = max(e - a for a, e in zip(self.offsets, self.offsets[1:]))
-        self.q: Optional[torch.Tensor] = None
-        self.k: Optional[torch.Tensor] = None
+        self._buffers: Dict[Tuple, torch.Tensor] = {}
         self._kept = []                # buffers that were replaced: captured graphs may hold them
 
-    def _buffer(self, old: Optional[torch.Tensor], x: torch.Tensor, rows: int) -> torch.Tensor:
-        """Room for ``rows`` rows of ``x`` [B, S, H, D]: the old one where it fits."""
+    def _buffer(self, name: str, x: torch.Tensor, rows: int) -> torch.Tensor:
+        """Room for ``rows`` rows of ``x`` [B, S, H, D]: one buffer for each type and
+        device, the old one where it fits."""
         n = x.shape[0] * rows * x.shape[2] * x.shape[3]
-        if old is None or old.numel() < n or old.dtype != x.dtype or old.device != x.device:
+        key = (name, x.dtype, x.device)
+        old = self._buffers.get(key)
+        if old is None or old.numel() < n:
             if old is not None:
                 self._kept.append(old)
-            return x.new_empty(n)
+                n = max(n, 2 * old.numel())          # what is kept stays below what is in use
+            old = self._buffers[key] = x.new_empty(n)
         return old
 
     def begin(self, qb: int, q_all: torch.Tensor, k: torch.Tensor, positions: torch.Tensor,
@@ -151,10 +154,8 @@ class RotatedInputs:
                 k.shape[1] != self.offsets[-1]:
             raise ValueError("an engine with rotary positions needs positions [1 or B, S, axes] of the whole sequence")
         block = q_all[:, a:e]
-        self.q = self._buffer(self.q, q_all, self.most)
-        self.k = self._buffer(self.k, k, k.shape[1])
-        q = self.q[:block.numel()].view(block.shape)
-        self._k = self.k[:k.numel()].view(k.shape)
+        q = self._buffer("q", q_all, self.most)[:block.numel()].view(block.shape)
+        self._k = self._buffer("k", k, k.shape[1])[:k.numel()].view(k.shape)
         self._src, self._pos, self._kw = k, positions, k_weight
         self._done = {qb}
         if e > a:

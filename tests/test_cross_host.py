@@ -62,3 +62,32 @@ def test_each_device_has_its_workspace(calls):
     z = torch.zeros(1, 3, 2, 64, dtype=BF16)
     op(z, x, x)
     assert log[-1][-1].numel() >= 1500 and len(op._kept) == 1 and op._kept[0] is used[0]
+
+
+def test_rotated_inputs_keep_a_buffer_of_each_type():
+    """Steps in bf16 and float32 in turn (states in float32 take both) use two
+    pairs of buffers, however many they are, and a larger batch keeps what it
+    replaces, within what it uses."""
+    from paper_2607_15650_amd.rotary import RotatedInputs
+    seen = []
+
+    def rotary(x, k, pos, qw=None, kw=None, q_out=None, k_out=None):
+        seen.append(q_out.data_ptr())
+
+    r = RotatedInputs(rotary, [0, 4, 12])
+    pos = torch.zeros(1, 12, 1, dtype=torch.int32)
+
+    def step(dtype, B=1):
+        x = torch.zeros(B, 12, 2, 64, dtype=dtype)
+        q = r.begin(0, x, x, pos, None, None)
+        k = r.keys([1, 1])
+        assert q.shape == (B, 4, 2, 64) and k.shape == x.shape and q.dtype == k.dtype == dtype
+        return q.data_ptr(), k.data_ptr()
+
+    first = [step(d) for d in (BF16, torch.float32)]
+    assert [step(d) for _ in range(3) for d in (BF16, torch.float32)] == first * 3 and not r._kept
+    for B in range(2, 12):
+        step(BF16, B)
+    in_use = sum(b.numel() * b.element_size() for b in r._buffers.values())
+    assert 0 < sum(b.numel() * b.element_size() for b in r._kept) <= in_use
+    assert {b.data_ptr() for b in r._kept} >= set(first[0])
