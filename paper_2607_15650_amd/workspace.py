@@ -4,7 +4,8 @@ ditango_attn_partition_states_ws balances a launch over the XCDs with queue
 counters in the workspace, and splits its last, partly filled round when
 given room for the partial states; the bytes depend on the shape, the
 selection and the device.  This holder asks the library for them once per
-(shape, selection) and keeps one device buffer that only grows.
+(shape, selection) and keeps one device buffer that only grows; one that became
+too small stays allocated, for graphs captured with it.
 """
 from __future__ import annotations
 
@@ -19,6 +20,7 @@ class AttnWorkspace:
     def __init__(self, device="cuda"):
         self.device = device
         self.buf: Optional[torch.Tensor] = None
+        self._kept = []
         self._bytes: Dict[Tuple, int] = {}
 
     def get(self, dtype: torch.dtype, B: int, H: int, D: int, q_len: int,
@@ -31,5 +33,9 @@ class AttnWorkspace:
         if n == 0:
             return None
         if self.buf is None or self.buf.numel() < n:
-            self.buf = torch.empty(n, dtype=torch.uint8, device=self.device)
+            size = n
+            if self.buf is not None:
+                self._kept.append(self.buf)
+                size = max(n, 2 * self.buf.numel())  # what is kept stays below what is in use
+            self.buf = torch.empty(size, dtype=torch.uint8, device=self.device)
         return self.buf

@@ -91,3 +91,19 @@ def test_rotated_inputs_keep_a_buffer_of_each_type():
     in_use = sum(b.numel() * b.element_size() for b in r._buffers.values())
     assert 0 < sum(b.numel() * b.element_size() for b in r._kept) <= in_use
     assert {b.data_ptr() for b in r._kept} >= set(first[0])
+
+
+def test_a_replaced_attention_workspace_stays_allocated(monkeypatch):
+    """A step that was captured holds the address of the workspace of its time."""
+    from paper_2607_15650_amd.workspace import AttnWorkspace
+    monkeypatch.setattr(api, "attn_workspace_bytes", lambda dtype, B, H, D, q_len, offsets, select: 256 * q_len)
+    ws = AttnWorkspace("cpu")
+    get = lambda n: ws.get(BF16, 1, 1, 64, n, [0, 1], [1])   # noqa: E731
+    small = get(1)
+    at = small.data_ptr()
+    assert get(1) is small
+    del small
+    held = [get(n) for n in range(2, 40)]
+    assert any(b.data_ptr() == at and b.numel() == 256 for b in ws._kept)
+    assert all(b.numel() >= 256 * n for n, b in zip(range(2, 40), held))
+    assert sum(b.numel() for b in ws._kept) <= ws.buf.numel()
