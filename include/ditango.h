@@ -321,7 +321,7 @@ ditango_status ditango_state_norms(
  *                Hk.
  *   D            64 or 128.
  *   q_len        at least 1; q_len * H below 2^31 - 1024.
- *   kv_len       keys of a sequence, 0 or more.
+ *   kv_len       keys of a sequence, 0 ... 2^31 - 2^20.
  *   kv_lens      device, [B] int32: the live keys of a sequence are its first
  *                kv_lens[b] (clamped to 0 ... kv_len); null: all.
  *   key_mask     device, [B][kv_len] bytes, non-zero = live; null: all.  With

@@ -261,7 +261,8 @@ __global__ __launch_bounds__(256) void cross_join_kernel(const CrossArgs a) {
   const int lane = threadIdx.x & (TEAM - 1), first = threadIdx.x & 63 & ~(TEAM - 1);
   const int b = (int)(r / a.q_len / a.H);
   // ranges of fixed length behind the sequence's end have not been written
-  const int parts = a.chunk > 0 ? min(a.split, (cross_keys(a, b) + a.chunk - 1) / a.chunk) : a.split;
+  // (n + chunk may pass 31 bits)
+  const int parts = a.chunk > 0 ? min(a.split, (int)(((uint32_t)cross_keys(a, b) + a.chunk - 1) / a.chunk)) : a.split;
   float mx = -INFINITY;
   bool bad = false;
   for (int p = lane; p < parts; p += TEAM) {
@@ -408,7 +409,7 @@ void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
       if (chunk < least) chunk = least;
       if (chunk < 256) chunk = 256;
       p->chunk = (int)((chunk + 127) / 128 * 128);
-      p->split = (a.kv_len + p->chunk - 1) / p->chunk;
+      p->split = (int)(((int64_t)a.kv_len + p->chunk - 1) / p->chunk);
     } else {
       p->chunk = a.kv_len;
     }

@@ -368,7 +368,9 @@ ditango_status cross_sizes(ditango_dtype dt, int B, int H, int Hk, int D, int64_
   if (!valid_dtype(dt)) return DITANGO_ERR_INVALID;
   if (B < 1 || H < 1 || Hk < 1 || q_len < 1 || kv_len < 0 || H % Hk != 0) return DITANGO_ERR_INVALID;
   if (D != 64 && D != 128) return DITANGO_ERR_UNSUPPORTED;
-  if (H > 32768 || q_len > (0x7fffffffLL - 1024) / H || kv_len > 0x7fffffffLL - 1024) return DITANGO_ERR_UNSUPPORTED;
+  // (the ends of key ranges, whole tiles or chunks, lie less than 2^20 keys
+  // behind the last one and are 32 bits too)
+  if (H > 32768 || q_len > (0x7fffffffLL - 1024) / H || kv_len > 0x80000000LL - (1 << 20)) return DITANGO_ERR_UNSUPPORTED;
   memset(a, 0, sizeof(*a));
   a->q_len = q_len;
   a->B = B;
