@@ -387,10 +387,13 @@ Estimate estimate_task(int64_t tasks, int64_t tiles, int D, int cus, double stat
 //  - kFew for up to 32 rows of a key/value head: 8 x 24 heads, 8 of them with
 //    keys, of one token against 16,384 keys 103 us (kRows 111), 12 heads against
 //    77 keys 4.7 us (5.4).
-//  - kResident where the keys fit LDS and every wave of it has one and a half
-//    blocks of rows at least: 9,450 rows x 40 heads against 256 keys 68 us (kRows
-//    81, kTask 78), 20,000 x 8 against 256 33 (39, 41), 14,850 x 48 at D=64
-//    against 512 112 (117, 137); but 9,450 x 12 against 256 33 (30, 29).
+//  - kResident where the keys fit LDS and its waves have work on them: one and a
+//    half blocks of rows each over all heads, and two and a half of each head,
+//    whose keys the waves wait for together: 9,450 rows x 40 heads against 256
+//    keys 68 us (kRows 81, kTask 78), 20,000 x 8 against 256 33 (39, 41), 14,850 x
+//    48 at D=64 against 512 112 (117, 137); but 9,450 x 12 against 256 33 (30,
+//    29), and 64 x 8,192 at D=64 against 256 242 (kRows 136), 512 x 8,192 519
+//    (422), 1,024 x 8,192 869 (856), 64 x 8,192 at D=128 against 320 441 (343).
 //  - kTask or kRows as estimated: 9,450 x 40 against 512 keys 113 us (kRows 125),
 //    against 1,024 183 (218); 700 x 24 against 512 19 (16).
 void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
@@ -415,8 +418,8 @@ void choose_form(const CrossArgs& a, int D, int cus, CrossPlan* p) {
     }
     return;
   }
-  if (a.kv_len <= cross_resident_keys(D) &&
-      2 * ((rows + 31) / 32) * heads >= 3 * (int64_t)cross_resident_waves(D) * cus) {
+  const int64_t blocks = (rows + 31) / 32, waves = cross_resident_waves(D);
+  if (a.kv_len <= cross_resident_keys(D) && 2 * blocks * heads >= 3 * waves * cus && 2 * blocks >= 5 * waves) {
     p->form = CrossPlan::kResident;
     return;
   }
