@@ -20,6 +20,11 @@
 //   position * freq in turns, float64, its fraction rounded to float32: the
 //   error is 2^-26 of a turn from the rounding and 2^-53 |position * freq|
 //   from the product, whatever the position.
+//
+// Range of the norm
+//   Squares leave float32 from 2^64 on, and below 2^-74 where eps is as small.
+//   Where a mean ends up near those ends the sum is taken again over elements
+//   scaled by a power of two, which the norm's factor undoes.
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -58,6 +63,13 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[VEC]) {
     for (int e = 0; e < VEC; ++e) v[e] = (T)x[e];
     __builtin_nontemporal_store(v, (V*)p);
   }
+}
+
+// Scale of the elements for a mean of squares (eps included) that lies near the
+// ends of float32, 1 otherwise.
+constexpr float kUp = 0x1p100f, kDown = 0x1p-80f;
+__device__ __forceinline__ float range_scale(float mean) {
+  return mean > 0x1p-100f && mean < 0x1p120f ? 1.f : mean < 1.f ? kUp : kDown;
 }
 
 // Units of a token that a thread holds: one of each tensor, or two of one.
@@ -110,6 +122,10 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
     for (int e = 0; e < VEC; ++e) q = __builtin_fmaf(x0[e], x0[e], __builtin_fmaf(x1[e], x1[e], q));
     return q;
   };
+  auto scaled = [&](float (&x0)[VEC], float (&x1)[VEC], float by) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x0[e] *= by, x1[e] *= by;
+  };
   // tensor and unit of held slot i; the first unit of tensor k that is not held
   const bool two = a.n == 2;
   auto tensor_of = [&](int i) { return two ? i : 0; };
@@ -146,6 +162,21 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
   // ---- the norm over the token's row: both tensors' sums of squares
   float scale[2] = {1.f, 1.f};
   if constexpr (NORM == 2) {
+    // (in all of a workgroup where its team is larger than a wave, in the team otherwise)
+    auto reduce = [&](float (&sq)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        for (int d = 1; d < (team < 64 ? team : 64); d <<= 1) sq[k] += __shfl_xor(sq[k], d, 64);
+        if (team > 64 && (tid & 63) == 0) sums[k][tid >> 6] = sq[k];
+      }
+    };
+    auto mean_of = [&](int k, float sq, float eps) {
+      if (team > 64) {
+        sq = 0.f;
+        for (int w = 0; w < (int)blockDim.x >> 6; ++w) sq += sums[k][w];
+      }
+      return sq / (float)(a.t[k].heads * D) + eps;
+    };
     float sq[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
@@ -164,19 +195,43 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
         const float q = squares(y0, y1);
         if (k == 0) sq[0] += q; else sq[1] += q;
       }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      for (int d = 1; d < (team < 64 ? team : 64); d <<= 1) sq[k] += __shfl_xor(sq[k], d, 64);
-      if (team > 64 && (tid & 63) == 0) sums[k][tid >> 6] = sq[k];
-    }
+    reduce(sq);
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (team > 64) {
-        sq[k] = 0.f;
-        for (int w = 0; w < (int)blockDim.x >> 6; ++w) sq[k] += sums[k][w];
+    for (int k = 0; k < 2; ++k)
+      if (k < a.n) scale[k] = mean_of(k, sq[k], a.eps);
+    const float by0 = range_scale(scale[0]), by1 = range_scale(scale[1]);
+    scale[0] = rsqrtf(scale[0]), scale[1] = rsqrtf(scale[1]);
+    if (by0 != 1.f || by1 != 1.f) {
+      // (the token read again: nothing of it has been written)
+      if (team > 64) __syncthreads();                 // every wave has read the sums
+      // (an element at a time: rare, and as few registers as the waves want)
+      int64_t s_again = s;
+      int b_again = b, u_again = in_team;
+      asm volatile("" : "+v"(s_again), "+v"(b_again), "+v"(u_again));
+      sq[0] = sq[1] = 0.f;
+#pragma unroll 1
+      for (int k = 0; k < a.n; ++k) {
+        const ditango_rotary_tensor& t = a.t[k];
+        const T* row = (const T*)t.x + b_again * t.x_strides[0] + s_again * t.x_strides[1];
+        float q = 0.f;
+#pragma unroll 1
+        for (int e = u_again; e < t.heads * D; e += team) {
+          const float x = (float)row[e / D * t.x_strides[2] + e % D] * (k == 0 ? by0 : by1);
+          q = __builtin_fmaf(x, x, q);
+        }
+        if (k == 0) sq[0] = q; else sq[1] = q;
       }
-      if (k < a.n) scale[k] = rsqrtf(sq[k] / (float)(a.t[k].heads * D) + a.eps);
+      reduce(sq);
+      if (team > 64) __syncthreads();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float by = k == 0 ? by0 : by1;
+        if (k < a.n && by != 1.f) {
+          const float r = rsqrtf(mean_of(k, sq[k], a.eps * by * by));
+          scale[k] = by < 1.f ? r * by : -r;          // (negative: of the elements times kUp)
+        }
+      }
     }
   } else {
     __syncthreads();
@@ -191,10 +246,22 @@ __global__ __launch_bounds__(1024) void rotary_kernel(const RotaryArgs a) {
       widen<T, VEC>(w0, v0);
       widen<T, VEC>(w1, v1);
       if constexpr (NORM == 1) {
-        float q = squares(y0, y1);
+        auto mean = [&](float eps) {
+          float q = squares(y0, y1);
 #pragma unroll
-        for (int d = 1; d < UD; d <<= 1) q += __shfl_xor(q, d, 64);
-        r = rsqrtf(q * (1.f / D) + a.eps);
+          for (int d = 1; d < UD; d <<= 1) q += __shfl_xor(q, d, 64);
+          return q * (1.f / D) + eps;
+        };
+        float m = mean(a.eps);
+        const float by = range_scale(m);                // (the same in all lanes of the head)
+        if (by != 1.f) {
+          scaled(y0, y1, by);
+          m = mean(a.eps * by * by);
+        }
+        r = rsqrtf(m);
+      } else if (r < 0.f) {
+        scaled(y0, y1, kUp);
+        r = -r;
       }
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
