@@ -117,3 +117,40 @@ def test_large_scores(gpu_lib, dtype, Lq, S, H, D, kind):
     assert int(clear.sum()) * 2 >= int((~ordinary).sum())
     one = (out - want).abs()[0] - 2.0 ** (-8 if dtype == BF16 else -22) * want.abs()[0] - 2.0 ** -40
     assert float(one.amax(-1)[clear].max()) <= 0 if bool(clear.any()) else True
+
+
+# shared heads, sequences of different lengths, and keys in LDS to the last byte of it (listed in the workspace)
+@pytest.mark.parametrize("kind", ["lens", "mask"])
+@pytest.mark.parametrize("dtype,B,Lq,S,H,Hk,D", [
+    (BF16, 2, 1, 3000, 12, 2, 128), (BF16, 3, 7, 100, 8, 4, 64), (BF16, 2, 70, 500, 6, 2, 128), (BF16, 2, 40, 4000, 6, 2, 64),
+    (BF16, 2, 2000, 320, 24, 8, 128), (BF16, 2, 4500, 640, 24, 24, 64), (BF16, 2, 1000, 900, 24, 8, 128),
+    (BF16, 2, 300, 3000, 12, 4, 64), (F32, 2, 300, 333, 12, 4, 128), (F32, 2, 2, 3000, 12, 4, 64)])
+def test_large_scores_and_values(gpu_lib, dtype, B, Lq, S, H, Hk, D, kind):
+    """Scores of 1e3 ... 1e30 whose largest is the next one's double at least, over
+    values of 1e38: in each row the value of one key, in float32 its product with
+    a few plane errors."""
+    from paper_2607_15650_amd.cross import CrossAttention
+    g = torch.Generator(device="cuda")
+    g.manual_seed(S + 1)
+    q = torch.zeros(B, Lq, H, D, device="cuda")
+    q[..., 5] = 10.0 ** torch.randint(3, 31, (B, Lq, H), generator=g, device="cuda").float()
+    q[:, ::2, :, 5] *= -1
+    # every key but two between -1/4 and 1/4; the largest is 1, the smallest -1
+    k = torch.zeros(B, S, Hk, D, device="cuda")
+    k[..., 5] = (torch.rand(B, S, Hk, generator=g, device="cuda") - 0.5) / 2
+    lens = torch.tensor([S - 5, S // 2, S][:B], dtype=torch.int32, device="cuda")
+    live = torch.arange(S, device="cuda") < lens[:, None]
+    if kind == "mask":
+        live = live & (torch.arange(S, device="cuda") % 5 != 3)
+    for b in range(B):
+        at = live[b].nonzero().flatten()
+        k[b, at[-2], :, 5], k[b, at[len(at) // 3], :, 5] = 1.0, -1.0
+    v = (torch.rand(B, S, Hk, D, generator=g, device="cuda") * 4 - 2) * 1e38
+    q, k, v = q.to(dtype), k.to(dtype), v.to(dtype)
+    out, lse = (x.double().cpu() for x in CrossAttention(1.3)(
+        q, k, v, **({"kv_lens": lens} if kind == "lens" else {"key_mask": live})))
+    want, el, _ = reference(q, k, v, 1.3, live, "cuda")
+    # scores are one product; the next key's probability is below exp(-1.3 * 1e3 * 3 / 4)
+    assert torch.isfinite(out).all()
+    assert float(((out - want).abs() - 2.0 ** (-8 if dtype == BF16 else -22) * want.abs()).max()) <= 2e38 * 2.0 ** -22
+    assert float(((lse - el).abs() - 2.0 ** -21 * el.abs()).max()) <= 0
