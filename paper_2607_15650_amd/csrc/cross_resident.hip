@@ -114,7 +114,8 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
       } else {
         const u32x4 desc = buffer_desc(base + (int64_t)i * BN * stride,
                                        (uint32_t)min((int64_t)(n - 1 - i * BN) * stride * 2 + C::ROWB, (int64_t)0x7fffffff));
-        dma_desc(desc, (uint32_t)r * (uint32_t)(stride * 2) + (uint32_t)unit * 16, dst);
+        // (places past the end: also where the keys' rows overlap)
+        dma_desc(desc, i * BN + r < n ? (uint32_t)r * (uint32_t)(stride * 2) + (uint32_t)unit * 16 : 0x80000000u, dst);
       }
     }
     auto load_queries = [&](int blk, int lane) {

@@ -154,3 +154,23 @@ def test_large_scores_and_values(gpu_lib, dtype, B, Lq, S, H, Hk, D, kind):
     assert torch.isfinite(out).all()
     assert float(((out - want).abs() - 2.0 ** (-8 if dtype == BF16 else -22) * want.abs()).max()) <= 2e38 * 2.0 ** -22
     assert float(((lse - el).abs() - 2.0 ** -21 * el.abs()).max()) <= 0
+
+
+@pytest.mark.parametrize("dtype,Lq,S,H,D", FORMS)
+def test_an_infinite_value_of_a_repeated_key(gpu_lib, dtype, Lq, S, H, D):
+    """One key and value for all places (a stride of 0): what lies past the last
+    place of a tile is nothing, not the value again with a weight of 0."""
+    from paper_2607_15650_amd.cross import CrossAttention
+    g = torch.Generator(device="cuda")
+    g.manual_seed(S)
+    q, k, v = (torch.randn(1, n, H, D, generator=g, device="cuda").to(dtype) for n in (Lq, 1, 1))
+    v[..., 3], v[..., 9] = math.inf, -math.inf
+    out, lse = CrossAttention(D ** -0.5)(q, k.expand(1, S, H, D), v.expand(1, S, H, D))
+    assert bool((out[..., 3] == math.inf).all()) and bool((out[..., 9] == -math.inf).all())
+    rest = torch.ones(D, dtype=torch.bool, device="cuda")
+    rest[3] = rest[9] = False
+    # equal probabilities, of one rounding: the value, and the output's rounding
+    d = (out - v)[..., rest].double().abs() - (2.0 ** (-7 if dtype == BF16 else -20)) * v[..., rest].double().abs()
+    assert float(d.max()) <= 2.0 ** -18
+    s = (q.double() * k.double()).sum(-1) * D ** -0.5 + math.log(S)
+    assert float((lse.double() - s.transpose(1, 2)).abs().max()) <= 1e-4
