@@ -24,8 +24,14 @@
 //
 // Rounding
 //   Products of bf16 values, accumulated in float32.  The probabilities go to
-//   bf16 for the second product (by at most 2^-8 of each; the row sum takes them
-//   before that), the output once more at its store.
+//   bf16 for the second product, by at most 2^-8 of each (the row sum takes them
+//   before that), the output once more at its store: half of the matrix core's
+//   work is that product, and a second bf16 plane of the probabilities would add
+//   as much again, here and in the kernels of many rows; the one of few rows,
+//   which waits for memory, has it (cross_few.hip).
+//
+// Range
+//   Rows whose sums or scores leave float32 are formed again (cross_tile.h).
 #include <math.h>
 
 #include <type_traits>
@@ -142,7 +148,7 @@ __global__ __launch_bounds__(C::NT, WPE) void cross_kernel(const CrossArgs) {
       if (st > 0 && key >= key_end) break;
       f32x16 sc = fr.scores(kt + st * 32 * C::ROWB, qf);
       if (key + 32 > key_end) mask_keys(sc, key_end - key, g);
-      bf16x8 pf[2];
+      bf16x8 pf[1][2];
       softmax_step<C::DB>(sc, pf, o, m, l, sl2, i + st == 0);
       fr.template values<false>(kt + C::NBUF * C::TILEB + st * 32 * C::ROWB, pf, o);
     }
@@ -346,10 +352,12 @@ hipError_t launch_rows(const CrossArgs& a, hipStream_t s) {
 }
 
 // Estimated times in us of a launch of the two kernels that share a head's keys
-// between many rows, with the split of the keys that is best for each.  Fitted
-// to 70 shapes of one card (100 ... 20,000 rows x 4 ... 40 heads, 77 ... 4,096
-// keys; most lie within 10 %), D=64 in brackets:
-//  - kRows: w workgroups share a compute unit; a tile of 64 keys 0.96 w + 0.45
+// between many rows, with the split of the keys that is best for each (D=64 in
+// brackets), fitted to launches of one card (100 ... 20,000 rows x 4 ... 40 heads,
+// 77 ... 4,096 keys):
+//  - kRows: w workgroups share a compute unit (one where there are fewer than
+//    compute units, between one and two a compute unit n of them count as
+//    (n + 2) / 2: some have a neighbour); a tile of 64 keys 0.96 w + 0.45
 //    (0.54 w + 0.25), and 3.2 w + 2 (1.5 w + 2.5) beside the tiles;
 //  - kTask: rounds of a task per compute unit, a tile 0.9 ... 1.4 (0.67 ...
 //    0.89) by how full the card is (its clock falls), 7.25 (5) beside a round's
@@ -357,6 +365,10 @@ hipError_t launch_rows(const CrossArgs& a, hipStream_t s) {
 //  - a split's partial states and their join 4, and 0.45 per MB: 2 x 4,095 rows
 //    x 12 heads against 2,048 keys 99 whole, 136 in two ranges; 300 x 40 against
 //    4,096 74 whole, 51 in three.
+// Lengths lie on the device: every sequence counts as kv_len keys.  A batch of
+// different lengths is dealt out better than that by kTask, and where the two lie
+// as near as 38.2 and 37.9 (2 x 4,095 rows x 12 heads, 512 keys) the choice is
+// not by what its lengths take (512 and 77: kTask 30).
 struct Estimate {
   double us;
   int split;

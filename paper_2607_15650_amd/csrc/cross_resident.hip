@@ -168,7 +168,7 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
           load_queries(blk + C::NW < last ? blk + C::NW : blk, lane);
           if ((i + 1) * 32 > n) mask_keys(sc, n - i * 32, g);
         }
-        bf16x8 pf[2];
+        bf16x8 pf[1][2];
         softmax_step<C::DB>(sc, pf, o, m, l, sl2, i == 0);
         fr.template values<true>(kt + C::TILEB, pf, o);
       }
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(C::NT, C::NW / 4) void cross_resident_kernel(const 
         const unsigned char* kt = smem + i / 2 * 2 * C::TILEB + i % 2 * 32 * C::ROWB;
         f32x16 sc = wr.scores(kt, qf);
         if ((i + 1) * 32 > n) mask_keys(sc, n - i * 32, wr.lane >> 5);
-        bf16x8 pf[2];
+        bf16x8 pf[1][2];
         wide_step<C::DB>(sc, pf, o, mx, l, sl2, low);
         wr.template values<true>(kt + C::TILEB, pf, o);
       }

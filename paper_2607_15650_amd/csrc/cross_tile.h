@@ -129,13 +129,16 @@ struct FragReader {
     return sc;
   }
   // O^T += V^T P^T of 32 keys
-  template <bool ORDERED>
-  __device__ __forceinline__ void values(const unsigned char* vt, const bf16x8 (&pf)[2], f32x16 (&o)[DB]) const {
+  template <bool ORDERED, int PLANES>
+  __device__ __forceinline__ void values(const unsigned char* vt, const bf16x8 (&pf)[PLANES][2], f32x16 (&o)[DB]) const {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-        o[db] = mfma32(ORDERED ? ordered_frag(vt, s, db) : value_frag(vt, s, db), pf[s], o[db]);
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 v = ORDERED ? ordered_frag(vt, s, db) : value_frag(vt, s, db);
+#pragma unroll
+        for (int j = PLANES - 1; j >= 0; --j) o[db] = mfma32(v, pf[j][s], o[db]);
+      }
   }
 };
 
@@ -146,14 +149,22 @@ __device__ __forceinline__ void mask_keys(f32x16& sc, int left, int g) {
     if (8 * (r >> 2) + 4 * g + (r & 3) >= left) sc[r] = -INFINITY;
 }
 
+// Probabilities of half a step's keys (8 of a lane) as PLANES bf16 planes: the
+// rounding of each, by at most 2^-8, and (PLANES = 2) that of what it leaves.
+template <int PLANES>
+__device__ __forceinline__ void round_probs(const f32x8& x, bf16x8 (&pf)[PLANES][2], int h) {
+  pf[0][h] = __builtin_convertvector(x, bf16x8);
+  if constexpr (PLANES == 2) pf[1][h] = __builtin_convertvector(x - __builtin_convertvector(pf[0][h], f32x8), bf16x8);
+}
+
 // Scores of 32 keys -> probabilities against the running maximum m, row sum l
 // (this lane's keys).  m is the first step's maximum, and raised only where a
 // lane's sum over a step then passes 2^40 or is not a number: below that
 // float32 holds the row sums, and the result does not depend on which m was
 // used.  It holds the outputs too while the values are below 2^80 or so;
 // out_of_range finds the rows where it does not.
-template <int DB>
-__device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], f32x16 (&o)[DB], float& m, float& l,
+template <int DB, int PLANES>
+__device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[PLANES][2], f32x16 (&o)[DB], float& m, float& l,
                                              float sl2, bool first) {
   float sum;
   auto raise = [&] {
@@ -181,7 +192,7 @@ __device__ __forceinline__ void softmax_step(const f32x16& sc, bf16x8 (&pf)[2], 
         x[e] = fast_exp2(__builtin_fmaf(sc[8 * h + e], sl2, -m));
         sum += x[e];
       }
-      pf[h] = __builtin_convertvector(x, bf16x8);
+      round_probs(x, pf, h);
     }
   };
   if (first) raise();
@@ -215,9 +226,10 @@ __device__ __forceinline__ bool out_of_range(const f32x16 (&o)[DB], float m) {
 // Scores of 32 keys -> probabilities 2^low exp2(scale (s - mx)) against the
 // maximum mx of the scores so far as they are: the largest is 2^low exactly
 // (attn_tile.h has low, by which sums over all keys stay below the values they
-// weigh).
+// weigh).  In one plane: the second, 0 or negative, would make NaN of an infinite
+// value.
 template <int DB>
-__device__ __forceinline__ void wide_step(const f32x16& sc, bf16x8 (&pf)[2], f32x16 (&o)[DB], float& mx, float& l,
+__device__ __forceinline__ void wide_step(const f32x16& sc, bf16x8 (&pf)[1][2], f32x16 (&o)[DB], float& mx, float& l,
                                           float sl2, float low) {
   float top = sc[0];
 #pragma unroll
@@ -237,7 +249,7 @@ __device__ __forceinline__ void wide_step(const f32x16& sc, bf16x8 (&pf)[2], f32
       x[e] = fast_exp2(__builtin_fmaf(sc[8 * h + e] - at, sl2, low));
       l += x[e];
     }
-    pf[h] = __builtin_convertvector(x, bf16x8);
+    round_probs(x, pf, h);
   }
 }
 // The state of 32 rows over keys [key_begin, key_end) in steps of 32 that lie
@@ -284,7 +296,7 @@ __device__ __forceinline__ void wide_pass(Args a, int b, int hk, int key_begin, 
     }
     f32x16 sc = fr.scores(own, qf);
     if (left < 32) mask_keys(sc, left, lane >> 5);
-    bf16x8 pf[2];
+    bf16x8 pf[1][2];
     wide_step<D / 32>(sc, pf, o, mx, l, sl2, low);
     fr.template values<false>(own + 32 * ROWB, pf, o);
   }

@@ -47,3 +47,24 @@ def test_elements(gpu_lib, B, Lq, S, H, Hk, D, dtype, kind):
         kw = {"key_mask": live}
     k, v = poison(k, v, live)
     check(CrossAttention(D ** -0.5)(q, k, v, **kw), q, k, v, live)
+
+
+@pytest.mark.parametrize("kind", ["all", "mask"])
+@pytest.mark.parametrize("B,Lq,S,H,Hk,D", [(1, 1, 77, 12, 12, 128), (2, 1, 4099, 8, 2, 64), (1, 1, 16384, 6, 2, 128),
+                                           (2, 8, 700, 8, 2, 64), (1, 32, 3000, 4, 4, 128)])
+def test_few_rows_round_once(gpu_lib, B, Lq, S, H, Hk, D, kind):
+    """Up to 32 rows of a key/value head: the probabilities are two bf16 planes, so
+    what is left is the output's rounding (2^-8), that of the second plane (2^-16 of
+    a probability) and float32's (2^-16 of the probabilities at scores of order 10,
+    2^-18 of the largest value for the sums)."""
+    from paper_2607_15650_amd.cross import CrossAttention
+    q, k, v = make(B, Lq, S, H, Hk, D, BF16, seed=Lq + S)
+    live, kw = torch.ones(B, S, dtype=torch.bool, device="cuda"), {}
+    if kind == "mask":
+        live = torch.arange(S, device="cuda").expand(B, S) % 3 != 1
+        kw = {"key_mask": live.contiguous()}
+    out, _ = CrossAttention(D ** -0.5)(q, k, v, **kw)
+    want, _, apart = reference(q, k, v, D ** -0.5, live, "cuda")
+    tol = 2.0 ** -8 * want.abs() + 2.0 ** -15 * apart + 2.0 ** -18 * float(v.abs().max())
+    over = (out.double().cpu() - want).abs() - tol
+    assert float(over.max()) <= 0, float(over.max())
