@@ -47,16 +47,19 @@ def flags():
     return CODEGEN_FLAGS + ["-I", INCLUDE, "-I", CSRC, "-Wall", "-Wno-unused-function"]
 
 
+_LAYER = ["layer.h", "kernel_lds.h"]
 # what a source includes besides internal.h and what that includes: shared and generated code
 INCLUDES = {"attn_bf16.hip": ["attn_tile.h", "attn_d128_loop.inc", "attn_d64_loop.inc"],
             "attn_bf16_any_q.hip": ["attn_bf16.hip", "attn_tile.h", "attn_d128_loop.inc", "attn_d64_loop.inc"],
-            "attn_f32.hip": ["attn_tile.h", "attn_f32_loop.h"],
-            "cross.hip": ["attn_tile.h", "cross_tile.h"],
-            "cross_few.hip": ["attn_tile.h", "cross_tile.h"],
-            "cross_resident.hip": ["attn_tile.h", "cross_tile.h"],
-            "cross_task.hip": ["attn_tile.h", "cross_tile.h", "cross_d128_loop.inc", "cross_d64_loop.inc"],
-            "cross_f32.hip": ["attn_tile.h", "attn_f32_loop.h"],
-            "rotary.hip": ["attn_tile.h"]}
+            "attn_f32.hip": ["attn_tile.h", "attn_f32_loop.h", "kernel_lds.h", "wide_range.h"],
+            "cross.hip": ["attn_tile.h", *_LAYER, "cross_tile.h", "wide_range.h"],
+            "cross_few.hip": ["attn_tile.h", *_LAYER, "cross_tile.h", "wide_range.h"],
+            "cross_resident.hip": ["attn_tile.h", *_LAYER, "cross_tile.h", "wide_range.h"],
+            "cross_task.hip": ["attn_tile.h", *_LAYER, "cross_tile.h", "wide_range.h", "cross_d128_loop.inc",
+                               "cross_d64_loop.inc"],
+            "cross_f32.hip": ["attn_tile.h", *_LAYER, "attn_f32_loop.h", "wide_range.h"],
+            "rotary.hip": ["attn_tile.h", *_LAYER],
+            "ditango_api.cpp": [*_LAYER]}
 
 
 def source_id(name: str) -> str:

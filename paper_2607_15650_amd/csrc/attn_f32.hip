@@ -51,6 +51,7 @@
 // tile and of the probabilities take 11 per pair of values).
 #include "attn_f32_loop.h"
 #include "internal.h"
+#include "kernel_lds.h"
 
 namespace ditango {
 namespace {

@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "attn_tile.h"
+#include "wide_range.h"
 
 namespace ditango {
 namespace {
@@ -101,7 +102,7 @@ struct ListedRows {
 // [t0, t1): unnormalised O^T, row maximum m (base 2, scaled) and the lane's
 // half of the row sum.  SPLIT: bf16 planes, otherwise the float32 MFMA, which
 // takes the probabilities as 2^low exp2(scale (s - max)) against the maximum as
-// it is (attn_tile.h; low 0 but for rows out of range).
+// it is (wide_range.h; low 0 but for rows out of range).
 // `ask`: the lanes whose query values need the latter.
 template <class C, bool SPLIT, class Rows>
 __device__ __forceinline__ void key_loop(const float* __restrict__ qrow, bool row_ok, const Rows& kg,

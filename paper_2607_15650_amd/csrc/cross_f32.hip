@@ -7,7 +7,7 @@
 // rows each, or (RW = 1) KW of them split the keys of its range, stage their own
 // tiles without barriers, and compose their partial states through LDS.
 #include "attn_f32_loop.h"
-#include "internal.h"
+#include "layer.h"
 
 namespace ditango {
 namespace {

@@ -10,7 +10,7 @@
 
 #include "attn_tile.h"
 #include "cross_tile.h"
-#include "internal.h"
+#include "layer.h"
 
 namespace ditango {
 namespace {

@@ -20,7 +20,7 @@
 #include "cross_d128_loop.inc"
 #include "cross_d64_loop.inc"
 #include "cross_tile.h"
-#include "internal.h"
+#include "layer.h"
 
 namespace ditango {
 namespace {

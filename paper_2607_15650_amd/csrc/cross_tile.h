@@ -3,7 +3,8 @@
 #pragma once
 
 #include "attn_tile.h"
-#include "internal.h"
+#include "layer.h"
+#include "wide_range.h"
 
 namespace ditango {
 namespace {
@@ -225,7 +226,7 @@ __device__ __forceinline__ bool out_of_range(const f32x16 (&o)[DB], float m) {
 
 // Scores of 32 keys -> probabilities 2^low exp2(scale (s - mx)) against the
 // maximum mx of the scores so far as they are: the largest is 2^low exactly
-// (attn_tile.h has low, by which sums over all keys stay below the values they
+// (wide_range.h has low, by which sums over all keys stay below the values they
 // weigh).  In one plane: the second, 0 or negative, would make NaN of an infinite
 // value.
 template <int DB>

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include "internal.h"
+#include "layer.h"
 
 using namespace ditango;
 

@@ -28,7 +28,7 @@
 #include <type_traits>
 
 #include "attn_tile.h"
-#include "internal.h"
+#include "layer.h"
 
 namespace ditango {
 namespace {
