@@ -83,6 +83,11 @@ typedef enum {
  * Slots whose select[j] == 0 are neither read nor written: they keep the state
  * cached at an earlier step, which is the reuse.  Selecting no partition is
  * valid and launches nothing.
+ *
+ * Range: with bf16 inputs, values below 2^80 and scores scale * q.k below 2^24;
+ * beyond, sums of unnormalised probabilities or a rounded maximum may leave
+ * float32 and OUT and LSE with them.  float32 inputs have no such limit: what
+ * float32 scores and a mean of the values can hold is computed.
  */
 ditango_status ditango_attn_partition_states(
     const void* q, const void* k, const void* v, ditango_dtype dt,
@@ -316,7 +321,11 @@ ditango_status ditango_state_norms(
  *                Addresses and strides are multiples of 16 bytes, and the
  *                strides between tokens of k and v below 2^24 elements
  *                (DITANGO_ERR_UNSUPPORTED otherwise).  k and v may be null
- *                when kv_len is 0.
+ *                when kv_len is 0.  All of these run; the fastest kernel of
+ *                many bf16 rows and keys takes K and V at one token stride of D
+ *                or more, a head's keys within 2 GiB, and queries whose token
+ *                and head strides are below 2^21 elements (head-major queries:
+ *                below 2^21 / D tokens); a masked call's keys are always so.
  *   H, Hk        query heads (at most 32768), key/value heads; H a multiple of
  *                Hk.
  *   D            64 or 128.
@@ -336,8 +345,15 @@ ditango_status ditango_state_norms(
  *                block over workgroups.  Calls that may overlap need one each.
  *
  * What lies in K and V at keys that are not live is never used, NaN included;
- * a row without live keys has OUT = 0 and LSE = -inf.  Results do not depend
- * on the order in which workgroups run.
+ * a row without live keys has OUT = 0 and LSE = -inf, whatever its query holds.
+ * Results do not depend on the order in which workgroups run.
+ *
+ * Precision: products of the inputs, accumulated in float32.  In bf16 the
+ * probabilities are rounded to bf16 (by at most 2^-8 of each) before they weigh
+ * V, and OUT once more (2^-8); up to 32 rows of a key/value head (a token, a
+ * handful) keep them in two planes, and only OUT's rounding is left.  Finite
+ * inputs give finite results as far as scores q.k, their product with scale *
+ * log2(e), and the weighted mean of the values fit float32.
  */
 ditango_status ditango_cross_attn(
     const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
@@ -362,7 +378,9 @@ size_t ditango_cross_attn_workspace_bytes(ditango_dtype dt, int B, int H, int Hk
  *     y0 = factor * (x^0 cos a - x^1 sin a),  y1 = factor * (x^0 sin a + x^1 cos a)
  * where a pair's elements are 2i and 2i + 1 (DITANGO_ROTARY_INTERLEAVED) or i
  * and i + rot_dim / 2 (DITANGO_ROTARY_HALF).  The others are x^.  Angles are
- * formed and reduced in float64, the rest is float32, rounded once.
+ * formed and reduced in float64, the rest is float32, rounded once.  The norm
+ * holds over the whole range of the values, also where their squares leave
+ * float32.
  *
  *   tensors      host, n_tensors (1 or 2: queries and keys of the same tokens)
  *                descriptions: x and y device, dtype `dt`, rows of D elements

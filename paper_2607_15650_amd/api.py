@@ -335,7 +335,7 @@ def cross_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float, 
     an encoder, H a multiple of Hk (ditango_cross_attn), into ``out`` [B, q_len,
     H, D] and ``lse`` [B, H, q_len].  q, k and v may be views with rows of their
     own distance (a packed projection); addresses and strides are multiples of
-    16 bytes.  ``kv_lens`` int32 [B]: the live keys of a sequence are its first
+    16 bytes, tokens of k and v less than 2^24 elements apart.  ``kv_lens`` int32 [B]: the live keys of a sequence are its first
     ones; ``key_mask`` bool or uint8 [B, kv_len], non-zero = live.  A masked call
     needs a ``workspace`` (uint8, 256-byte aligned) of
     cross_attn_workspace_bytes(...) bytes, another one splits the keys of a short

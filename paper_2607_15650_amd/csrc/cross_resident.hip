@@ -3,9 +3,16 @@
 //
 // A prompt's states of one head are small: 256 keys at D=64 take 64 KB.  A
 // workgroup per compute unit, of 12 waves (D=64: 16, as many as their registers
-// allow), loads them once and its waves walk over blocks of query rows by themselves, without a barrier: while one
-// wave of a SIMD takes exponentials the others' products run.  The next
-// block's queries are on their way from the last use of this one's on.
+// allow), loads them once and its waves walk over blocks of query rows by
+// themselves, without a barrier: while one wave of a SIMD takes exponentials the
+// others' products run.  The next block's queries are on their way from the last
+// use of this one's on.
+//
+// 14,850 rows x 48 heads at D=64 against 256 of 333 keys: 79 us, the matrix core
+// busy 28 % of it and the vector unit about half (exponentials, conversions,
+// sums); a workgroup's 87 blocks of a share are 5.4 rounds of its waves, run as
+// six, and at a change of head all of them wait for the mask's list and the new
+// keys.  9,450 x 40 at D=128 against 256: 74-77 us, the same way.
 #include <type_traits>
 
 #include "attn_tile.h"

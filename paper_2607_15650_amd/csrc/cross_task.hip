@@ -12,8 +12,9 @@
 //
 // Bound by the matrix core's power and, between tasks, by latency: of 32.8
 // thousand cycles of a task of 512 keys 24.2 are the key loop (16.4 of them
-// MFMAs), 9,450 rows x 40 heads take 112-120 us (840 TFLOP/s); 8,192 x 24 heads
-// against 4,099 keys of 8 306-338 (1.22-1.35 PFLOP/s).
+// MFMAs), 9,450 rows x 40 heads take 117-122 us (830 TFLOP/s); 8,192 x 24 heads
+// against 4,099 keys of 8 311-328 (1.26-1.33 PFLOP/s; 322-379 under a profiler,
+// at lower clocks).
 #include <type_traits>
 
 #include "attn_tile.h"
@@ -47,7 +48,7 @@ struct TaskCfg {
 };
 
 // Bound on a lane's row sum below which the fast loop's result is the checked
-// loop's (attn_bf16.hip).
+// loop's (attn_bf16.hip), as long as the outputs are in range (cross_tile.h).
 constexpr float kRowSumBound = 1099511627776.0f;   // 2^40
 
 // x / d for wave-uniform 0 <= x < 2^31, with 2^32 / d rounded down (d = 1:
