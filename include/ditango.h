@@ -352,8 +352,8 @@ ditango_status ditango_state_norms(
  * probabilities are rounded to bf16 (by at most 2^-8 of each) before they weigh
  * V, and OUT once more (2^-8); up to 32 rows of a key/value head (a token, a
  * handful) keep them in two planes, and only OUT's rounding is left.  Finite
- * inputs give finite results as far as scores q.k, their product with scale *
- * log2(e), and the weighted mean of the values fit float32.
+ * inputs give finite results as far as scores q.k and their product with scale *
+ * log2(e) fit float32, and the weighted mean of the values, as rounded, the type.
  */
 ditango_status ditango_cross_attn(
     const void* q, const int64_t* q_strides, const void* k, const int64_t* k_strides,
